@@ -1,0 +1,169 @@
+// kv_extend.hip -- pages, slots and positions of a batch's new tokens, from
+// lengths that stay on the GPU (include/eb_attention.h, eb_kv_extend).
+//
+// With a_b new tokens and n_b new pages of sequence b, row r belongs to the
+// sequence with start_b <= r < start_b + a_b, start = exclusive sums of a, and
+// its token is at p = cached_b + r - start_b.  The i-th new page of b is number
+// sum_{c < b} n_c + i from the top of the stack.
+//
+// One launch: every workgroup sums over the whole batch itself (8 bytes per
+// sequence, from L2) and keeps the sums in LDS, then fills its own rows; a row
+// that begins a page writes the table's entry for it.  So no workgroup waits
+// for another, and pages taken in this call are read from the stack, never
+// from table entries that another workgroup writes.  The work is latency: one
+// read of the lengths, 12 scan steps per 256 sequences, a binary search in LDS
+// per row and one dependent read of the page.
+#include <hip/hip_runtime.h>
+
+#include "attention.h"
+
+namespace eb {
+namespace {
+
+constexpr int kThreads = 256;
+
+__device__ inline int64_t nonneg(int32_t v) { return v > 0 ? v : 0; }
+
+// Inclusive sum over the workgroup's threads; *total is the sum of all.
+__device__ inline int64_t block_scan(int64_t v, int64_t *red, int64_t *total) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const int64_t u = __shfl_up(v, d);
+    if (lane >= d) v += u;
+  }
+  if (lane == 63) red[wave] = v;
+  __syncthreads();
+  int64_t before = 0, all = 0;
+#pragma unroll
+  for (int w = 0; w < kThreads / 64; ++w) {
+    if (w < wave) before += red[w];
+    all += red[w];
+  }
+  __syncthreads();
+  *total = all;
+  return v + before;
+}
+
+__global__ void __launch_bounds__(kThreads) kv_extend_kernel(eb_kv_extend_op o, int page_shift) {
+  extern __shared__ int32_t lds[];
+  int32_t *start = lds;                // [batch + 1], at most o.rows
+  int32_t *taken = lds + o.batch + 1;  // [batch + 1], at most 2^31 - 1
+  __shared__ int64_t red[kThreads / 64];
+  const int32_t page = o.page;
+  const int64_t capacity = (int64_t)o.table_stride << page_shift;  // tokens of a table row
+  const bool first = blockIdx.x == 0;
+  const int64_t n_free = min(nonneg(o.n_free[0]), (int64_t)o.free_capacity);
+
+  int64_t rows_before = 0, pages_before = 0;
+  for (int32_t b0 = 0; b0 < o.batch; b0 += kThreads) {
+    const int32_t b = b0 + (int32_t)threadIdx.x;
+    const bool ok = b < o.batch;
+    const int64_t have = ok ? nonneg(o.cached[b]) : 0, add = ok ? nonneg(o.added[b]) : 0;
+    const int64_t total = min(have + add, capacity), held = (min(have, capacity) + page - 1) >> page_shift;
+    const int64_t need = ok ? ((total + page - 1) >> page_shift) - held : 0;
+    int64_t rows_all, pages_all;
+    const int64_t rows_in = block_scan(add, red, &rows_all);
+    const int64_t pages_in = block_scan(need, red, &pages_all);
+    if (ok) {
+      start[b] = (int32_t)min(rows_before + rows_in - add, (int64_t)o.rows);
+      taken[b] = (int32_t)min(pages_before + pages_in - need, (int64_t)0x7fffffff);
+      if (first) {
+        o.q_start[b] = start[b];
+        o.kv_len[b] = (int32_t)total;
+      }
+    }
+    rows_before += rows_all;
+    pages_before += pages_all;
+  }
+  if (threadIdx.x == 0) {
+    start[o.batch] = (int32_t)min(rows_before, (int64_t)o.rows);
+    taken[o.batch] = (int32_t)min(pages_before, (int64_t)0x7fffffff);
+    if (first) {
+      o.q_start[o.batch] = start[o.batch];
+      o.n_free_out[0] = (int32_t)max(n_free - pages_before, (int64_t)0);
+    }
+  }
+  __syncthreads();
+
+  // The last sequence b in [0, batch) with sums[b] <= v (sums ascend).
+  auto find = [&](const int32_t *sums, int32_t v) {
+    int32_t lo = 0, hi = o.batch;
+    while (hi - lo > 1) {
+      const int32_t mid = (lo + hi) >> 1;
+      if (sums[mid] <= v)
+        lo = mid;
+      else
+        hi = mid;
+    }
+    return lo;
+  };
+  auto valid = [&](int32_t p) { return p >= 0 && p < o.pages ? p : -1; };
+  auto fresh = [&](int64_t nth) { return nth < n_free ? valid(o.free_pages[n_free - 1 - nth]) : -1; };
+
+  const int32_t live = start[o.batch];
+  for (int64_t r = (int64_t)blockIdx.x * kThreads + threadIdx.x; r < o.rows;
+       r += (int64_t)gridDim.x * kThreads) {
+    int32_t slot = -1, pos = 0;
+    if (r < live) {
+      const int32_t b = find(start, (int32_t)r);
+      const int64_t have = nonneg(o.cached[b]), p = have + r - start[b];
+      pos = (int32_t)min(p, (int64_t)0x7fffffff);
+      if (p < capacity) {
+        const int64_t held = (have + page - 1) >> page_shift, at = p >> page_shift;
+        int32_t *entry = o.table + (int64_t)b * o.table_stride + at;
+        int32_t id;
+        if (at < held) {
+          id = valid(*entry);
+        } else {
+          id = fresh(taken[b] + at - held);
+          if ((p & (page - 1)) == 0) *entry = id;
+        }
+        if (id >= 0) slot = (id << page_shift) + (int32_t)(p & (page - 1));
+      }
+    }
+    o.slots[r] = slot;
+    o.positions[r] = pos;
+  }
+  if (!first) return;
+
+  // Tokens without a page: those past a table row, those on a held page that is
+  // missing, those on new pages that the stack does not have, and those on new
+  // pages whose entry in the stack is no page.
+  int64_t miss = 0;
+  for (int32_t b = threadIdx.x; b < o.batch; b += kThreads) {
+    const int64_t have = nonneg(o.cached[b]), all = have + nonneg(o.added[b]);
+    const int64_t total = min(all, capacity);
+    miss += max(all - max(have, capacity), (int64_t)0);
+    const int64_t held = (min(have, capacity) + page - 1) >> page_shift;
+    const int64_t end = min(total, held << page_shift);
+    if (have < end && valid(o.table[(int64_t)b * o.table_stride + held - 1]) < 0) miss += end - have;
+    const int64_t got = max(n_free - taken[b], (int64_t)0);
+    miss += max(total - max(have, (held + got) << page_shift), (int64_t)0);
+  }
+  const int32_t took = (int32_t)min((int64_t)taken[o.batch], n_free);
+  for (int32_t i = threadIdx.x; i < took; i += kThreads) {
+    if (fresh(i) >= 0) continue;
+    const int32_t b = find(taken, i);
+    const int64_t have = nonneg(o.cached[b]), total = min(have + nonneg(o.added[b]), capacity);
+    const int64_t at = ((have + page - 1) >> page_shift) + i - taken[b];
+    miss += min((at + 1) << page_shift, total) - (at << page_shift);
+  }
+  int64_t all;
+  block_scan(miss, red, &all);
+  if (threadIdx.x == 0) o.short_rows[0] = (int32_t)min(all, (int64_t)0x7fffffff);
+}
+
+}  // namespace
+
+hipError_t launch_kv_extend(const eb_kv_extend_op &o, hipStream_t s) {
+  const int shift = __builtin_ctz((unsigned)o.page);
+  // a row per thread up to 2 workgroups per CU's worth of rows, then several
+  const int64_t wgs = ((int64_t)o.rows + kThreads - 1) / kThreads;
+  const unsigned grid = (unsigned)(wgs < 1 ? 1 : (wgs > 512 ? 512 : wgs));
+  const size_t lds = sizeof(int32_t) * 2 * (size_t)(o.batch + 1);
+  kv_extend_kernel<<<grid, kThreads, lds, s>>>(o, shift);
+  return hipGetLastError();
+}
+
+}  // namespace eb

@@ -6,7 +6,8 @@ memory), passes raw device pointers and the current HIP stream, and turns
 status codes into exceptions.  It raises at import time if libeb.so has not
 been built (there is no fallback path).
 
-Names follow the C ABI in include/eb.h and include/eb_tuning.h.
+Names follow the C ABI in include/eb.h, include/eb_tuning.h, include/eb_multirate.h
+and include/eb_attention.h.
 """
 from __future__ import annotations
 
@@ -456,3 +457,281 @@ def multirate_launches(mods: ctypes.Array, tick: int) -> int:
     if n < 0:
         raise EBError(n, "eb_multirate_launches")
     return n
+
+
+# ---------------------------------------------------------------------------
+# The steps between a layer's QKV and O projections (include/eb_attention.h).
+# Their ops are packed into bytes, as those of single projections are.
+# ---------------------------------------------------------------------------
+
+EB_ROT_HALF = 0
+EB_ROT_ADJACENT = 1
+EB_MASK_CAUSAL = 0
+EB_MASK_FULL = 1
+STYLES = {"half": EB_ROT_HALF, "adjacent": EB_ROT_ADJACENT}
+MASKS = {"causal": EB_MASK_CAUSAL, "full": EB_MASK_FULL}
+
+
+class eb_kv_cache(ctypes.Structure):
+    _fields_ = [("k", _vp), ("v", _vp), ("type", _i32), ("heads", _i32), ("dim", _i32),
+                ("page", _i32), ("pages", _i32), ("reserved", _i32)]
+
+
+class eb_kv_extend_op(ctypes.Structure):
+    _fields_ = [(n, _vp) for n in ("cached", "added", "table", "free_pages", "n_free", "n_free_out",
+                                   "q_start", "kv_len", "slots", "positions", "short_rows")] + \
+               [(n, _i32) for n in ("batch", "rows", "page", "pages", "table_stride", "free_capacity")]
+
+
+class eb_rope_append_op(ctypes.Structure):
+    _fields_ = [("cache", eb_kv_cache)] + \
+               [(n, _vp) for n in ("qkv", "q_out", "slots", "positions", "freqs", "q_norm", "k_norm")] + \
+               [(n, _i64) for n in ("qkv_stride", "q_stride", "pos_stride")] + \
+               [(n, _i32) for n in ("qkv_type", "q_heads", "rows", "rot", "style", "n_axes")] + \
+               [("sections", _i32 * 3), ("norm_eps", ctypes.c_float)]
+
+
+class eb_attention_op(ctypes.Structure):
+    _fields_ = [("cache", eb_kv_cache)] + \
+               [(n, _vp) for n in ("q", "out", "table", "q_start", "kv_len", "prefix")] + \
+               [("q_stride", _i64), ("out_stride", _i64)] + \
+               [(n, _i32) for n in ("rows", "batch", "q_heads", "table_stride", "max_new", "max_kv",
+                                    "mask", "window")] + \
+               [("scale", ctypes.c_float), ("softcap", ctypes.c_float)]
+
+
+_CACHE = "PPiiiiii"
+_PACK_EXTEND = struct.Struct("11P6i")
+_PACK_ROPE = struct.Struct(_CACHE + "7P3q6i3if")
+_PACK_ATTN = struct.Struct(_CACHE + "6P2q8i2f")
+for _s, _c in ((_PACK_EXTEND, eb_kv_extend_op), (_PACK_ROPE, eb_rope_append_op),
+               (_PACK_ATTN, eb_attention_op)):
+    assert _s.size == ctypes.sizeof(_c)
+
+lib.eb_kv_extend.restype = _i32
+lib.eb_kv_extend.argtypes = [ctypes.POINTER(eb_kv_extend_op), _vp]
+lib.eb_rope_append.restype = _i32
+lib.eb_rope_append.argtypes = [ctypes.POINTER(eb_rope_append_op), _vp]
+lib.eb_attention_workspace_bytes.restype = ctypes.c_size_t
+lib.eb_attention_workspace_bytes.argtypes = [ctypes.POINTER(eb_attention_op)]
+lib.eb_attention.restype = _i32
+lib.eb_attention.argtypes = [ctypes.POINTER(eb_attention_op), _vp, ctypes.c_size_t, _vp]
+_kv_extend, _rope_append, _attention = _raw.eb_kv_extend, _raw.eb_rope_append, _raw.eb_attention
+_attention_ws = _raw.eb_attention_workspace_bytes
+for _f in (_kv_extend, _rope_append):
+    _f.restype, _f.argtypes = _i32, [ctypes.c_char_p, _vp]
+_attention.restype, _attention.argtypes = _i32, [ctypes.c_char_p, _vp, ctypes.c_size_t, _vp]
+_attention_ws.restype, _attention_ws.argtypes = ctypes.c_size_t, [ctypes.c_char_p]
+_ATTN_WS_BYTES = {}  # at most 4096 entries
+
+
+def _need(ok: bool, what: str) -> None:
+    """Checks of what only the binding can see: types, shapes and devices of tensors."""
+    if not ok:
+        raise ValueError(what)
+
+
+def _ints(name: str, t: torch.Tensor, device, *shape) -> int:
+    _need(t.dtype == torch.int32 and t.device == device and t.is_contiguous()
+          and (not shape or tuple(t.shape) == shape),
+          f"{name}: a contiguous int32 tensor on {device}" + (f" of shape {shape}" if shape else ""))
+    return t.data_ptr()
+
+
+def _floats(name: str, t: torch.Tensor | None, device, n: int) -> int:
+    if t is None:
+        return 0
+    _need(t.dtype == torch.float32 and t.device == device and t.is_contiguous() and t.numel() == n,
+          f"{name}: {n} contiguous float32 values on {device}")
+    return t.data_ptr()
+
+
+def _rows(name: str, t: torch.Tensor, device, dtype, width: int) -> int:
+    """Stride between the rows of t, whose first row axis may be strided."""
+    inner = t.shape[1:].numel()
+    _need(t.device == device and t.dtype == dtype and t.dim() >= 2 and inner == width
+          and (t.shape[0] == 0 or t[0].is_contiguous()),
+          f"{name}: rows of {width} {dtype} values on {device}")
+    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), width)
+
+
+class _on:
+    """Makes `device` current for a launch, where it is not."""
+
+    def __init__(self, device):
+        self.to, self.was = device.index, torch.cuda.current_device()
+
+    def __enter__(self):
+        if self.to != self.was:
+            torch.cuda.set_device(self.to)
+        return _raw_stream(self.to)
+
+    def __exit__(self, *exc):
+        if self.to != self.was:
+            torch.cuda.set_device(self.was)
+
+
+class KVCache:
+    """The keys and values of one layer: k, v [pages, heads, page, dim] of
+    binary16 or bfloat16, caller-owned."""
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor):
+        _need(k.is_cuda and k.dim() == 4 and k.shape == v.shape and k.dtype == v.dtype
+              and k.device == v.device and k.is_contiguous() and v.is_contiguous()
+              and k.dtype in (torch.float16, torch.bfloat16),
+              "k and v: contiguous [pages, heads, page, dim] of float16 or bfloat16 on one GPU")
+        self.k, self.v = k, v
+        self.pages, self.heads, self.page, self.dim = k.shape
+
+    @property
+    def device(self):
+        return self.k.device
+
+    @property
+    def dtype(self):
+        return self.k.dtype
+
+    def fields(self) -> tuple:
+        return (self.k.data_ptr(), self.v.data_ptr(), DTYPES[self.k.dtype], self.heads, self.dim,
+                self.page, self.pages, 0)
+
+
+def empty_kv_cache(pages: int, page: int, heads: int, dim: int, dtype=torch.bfloat16,
+                   device="cuda") -> KVCache:
+    shape = (pages, heads, page, dim)
+    return KVCache(torch.empty(shape, dtype=dtype, device=device),
+                   torch.empty(shape, dtype=dtype, device=device))
+
+
+class KVBatch:
+    """What eb_kv_extend writes beside the block table (int32, on the GPU)."""
+
+    def __init__(self, batch: int, rows: int, device):
+        # one buffer: q_start, kv_len, slots, positions, pages left, tokens without a page
+        sizes = (batch + 1, batch, rows, rows, 1, 1)
+        buf = torch.empty(sum(sizes), dtype=torch.int32, device=device)
+        self.q_start, self.kv_len, self.slots, self.positions, self.n_free, self.short = \
+            buf.split(sizes)
+
+
+def kv_extend(table: torch.Tensor, cached: torch.Tensor, added: torch.Tensor,
+              free_pages: torch.Tensor, n_free: torch.Tensor, page: int, pages: int, rows: int,
+              out: KVBatch | None = None) -> KVBatch:
+    """New tokens join the sequences of a batch (eb_kv_extend): `table`
+    [batch, stride] gets the new pages' entries in place; the lengths, slots and
+    positions of a step of `rows` rows are returned.  n_free stays as it was:
+    the pages left are the result's n_free."""
+    dev = table.device
+    _need(table.is_cuda and table.dim() == 2, "table: [batch, stride] on a GPU")
+    batch, stride = table.shape
+    out = out or KVBatch(batch, rows, dev)
+    op = _PACK_EXTEND.pack(
+        _ints("cached", cached, dev, batch), _ints("added", added, dev, batch),
+        _ints("table", table, dev), _ints("free_pages", free_pages, dev),
+        _ints("n_free", n_free, dev, 1), _ints("n_free", out.n_free, dev, 1),
+        _ints("q_start", out.q_start, dev, batch + 1), _ints("kv_len", out.kv_len, dev, batch),
+        _ints("slots", out.slots, dev, rows), _ints("positions", out.positions, dev, rows),
+        _ints("short", out.short, dev, 1), batch, rows, page, pages, stride, free_pages.numel())
+    with _on(dev) as stream:
+        _check(_kv_extend(op, stream), "eb_kv_extend")
+    return out
+
+
+def rope_append(qkv: torch.Tensor, cache: KVCache, slots: torch.Tensor, positions: torch.Tensor | None,
+                freqs: torch.Tensor | None, q_heads: int, q_norm: torch.Tensor | None = None,
+                k_norm: torch.Tensor | None = None, eps: float = 0.0, style: str = "half",
+                sections=None, out: torch.Tensor | None = None) -> torch.Tensor:
+    """Head norms, rotation and the cache write of one layer (eb_rope_append):
+    qkv [rows, (q_heads + 2 heads) * dim] -> queries [rows, q_heads, dim]; keys
+    and values go to `cache` at `slots`.  positions: [rows], or [axes, rows] with
+    `sections` (rotated pairs along each axis); freqs: radians per position of
+    each rotated pair, 2 * len(freqs) elements of a head being rotated."""
+    dev, dim = cache.device, cache.dim
+    rows = qkv.shape[0]
+    stride = _rows("qkv", qkv, dev, qkv.dtype, (q_heads + 2 * cache.heads) * dim)
+    _need(qkv.dtype in DTYPES, "qkv: float32, float16 or bfloat16")
+    if out is None:
+        out = torch.empty((rows, q_heads, dim), dtype=cache.dtype, device=dev)
+    _need(out.shape[0] == rows, "out: a row for each row of qkv")
+    q_stride = _rows("out", out, dev, cache.dtype, q_heads * dim)
+    half = freqs.numel() if freqs is not None else 0
+    axes, pos, pos_stride = 1, 0, 0
+    if half:
+        _need(positions is not None and positions.dim() <= 2 and positions.shape[-1] == rows,
+              "positions: [rows] or [axes, rows]")
+        axes = positions.shape[0] if positions.dim() == 2 else 1
+        pos, pos_stride = _ints("positions", positions, dev), rows
+    sections = tuple(sections) if sections is not None else (half,)
+    _need(len(sections) == axes and axes <= 3, "sections: rotated pairs for each of up to 3 axes")
+    op = _PACK_ROPE.pack(
+        *cache.fields(), qkv.data_ptr(), out.data_ptr(), _ints("slots", slots, dev, rows), pos,
+        _floats("freqs", freqs, dev, half), _floats("q_norm", q_norm, dev, dim),
+        _floats("k_norm", k_norm, dev, dim), stride, q_stride, pos_stride, DTYPES[qkv.dtype], q_heads,
+        rows, 2 * half, STYLES[style], axes, *(sections + (0, 0))[:3], float(eps))
+    with _on(dev) as stream:
+        _check(_rope_append(op, stream), "eb_rope_append")
+    return out
+
+
+def attention(q: torch.Tensor, cache: KVCache, table: torch.Tensor, q_start: torch.Tensor,
+              kv_len: torch.Tensor, max_new: int, max_kv: int, mask: str = "causal",
+              prefix: torch.Tensor | None = None, window: int = 0, softcap: float = 0.0,
+              scale: float | None = None, out: torch.Tensor | None = None,
+              workspace: torch.Tensor | None = None) -> torch.Tensor:
+    """Attention of a batch's new tokens over the paged cache (eb_attention):
+    q [rows, q_heads, dim] -> the same shape.  scale: dim ** -0.5 where not
+    given.  workspace: a uint8 tensor of attention_workspace_bytes bytes; without
+    one the call takes one from scratch(), or, under graph capture, a fresh one
+    that belongs to the graph."""
+    dev, dim = cache.device, cache.dim
+    _need(q.dim() == 3 and q.shape[2] == dim, "q: [rows, q_heads, dim]")
+    rows, q_heads, _ = q.shape
+    _need(table.dim() == 2, "table: [batch, stride]")
+    batch, table_stride = table.shape
+    q_stride = _rows("q", q, dev, cache.dtype, q_heads * dim)
+    if out is None:
+        out = torch.empty((rows, q_heads, dim), dtype=cache.dtype, device=dev)
+    _need(out.shape[0] == rows, "out: a row for each row of q")
+    out_stride = _rows("out", out, dev, cache.dtype, q_heads * dim)
+    if scale is None:
+        scale = dim ** -0.5
+    op = _PACK_ATTN.pack(
+        *cache.fields(), q.data_ptr(), out.data_ptr(), _ints("table", table, dev),
+        _ints("q_start", q_start, dev, batch + 1), _ints("kv_len", kv_len, dev, batch),
+        _ints("prefix", prefix, dev, batch) if prefix is not None else 0, q_stride, out_stride, rows,
+        batch, q_heads, table_stride, max_new, max_kv, MASKS[mask], window, scale, softcap)
+    with _on(dev) as stream:
+        if workspace is None:
+            # what the size depends on (the current device's CU count too)
+            key = (rows, batch, q_heads, cache.heads, dim, max_new, max_kv, mask, dev.index)
+            nbytes = _ATTN_WS_BYTES.get(key)
+            if nbytes is None:
+                nbytes = _attention_ws(op)  # 0 too for a call that will be refused
+            if not nbytes:
+                workspace = None
+            elif torch.cuda.is_current_stream_capturing():
+                workspace = torch.empty(nbytes, dtype=torch.uint8, device=dev)
+            else:
+                workspace = scratch(dev, nbytes)
+        else:
+            key = nbytes = None
+            _need(workspace.dtype == torch.uint8 and workspace.device == dev
+                  and workspace.is_contiguous(), f"workspace: contiguous uint8 on {dev}")
+        _check(_attention(op, workspace.data_ptr() if workspace is not None else None,
+                          workspace.numel() if workspace is not None else 0, stream), "eb_attention")
+    if key is not None and key not in _ATTN_WS_BYTES:
+        if len(_ATTN_WS_BYTES) >= 4096:
+            _ATTN_WS_BYTES.clear()
+        _ATTN_WS_BYTES[key] = nbytes
+    return out
+
+
+def attention_workspace_bytes(q_shape, cache: KVCache, batch: int, table_stride: int, max_new: int,
+                              max_kv: int, mask: str = "causal") -> int:
+    """Bytes of workspace that attention() needs for queries of q_shape."""
+    rows, q_heads, dim = q_shape
+    w, stand_in = q_heads * dim, cache.k.data_ptr()  # pointers are only checked for alignment
+    op = _PACK_ATTN.pack(*cache.fields(), stand_in, stand_in, stand_in, stand_in, stand_in, 0, w, w, rows,
+                         batch, q_heads, table_stride, max_new, max_kv, MASKS[mask], 0, 1.0, 0.0)
+    with _on(cache.device):
+        return int(_attention_ws(op))
