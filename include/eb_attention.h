@@ -83,7 +83,7 @@ typedef struct {
   int32_t rows;              /* 0 .. 2^24: the rows that the step runs with */
   int32_t page;              /* as in eb_kv_cache */
   int32_t pages;
-  int32_t table_stride;      /* >= 1, table_stride * page <= 2^31 - 1 */
+  int32_t table_stride;      /* >= 1, table_stride * page <= 2^30 */
   int32_t free_capacity;     /* >= 0 */
 } eb_kv_extend_op;
 
@@ -176,7 +176,7 @@ typedef struct {
   int32_t rows;           /* 0 .. 2^24 */
   int32_t batch;          /* 1 .. 4096 */
   int32_t q_heads;        /* a multiple of the cache's heads, at most 4096 */
-  int32_t table_stride;   /* >= 1, table_stride * page <= 2^31 - 1 */
+  int32_t table_stride;   /* >= 1, table_stride * page <= 2^30 */
   int32_t max_new;        /* >= 1 */
   int32_t max_kv;         /* >= 1 */
   int32_t mask;           /* EB_MASK_CAUSAL or EB_MASK_FULL */

@@ -25,7 +25,8 @@ ARCH = "gfx950"
 SOURCES = ["eb_api.cpp", "eb_multirate.cpp", "quantize.hip", "gemv.hip", "norm.hip", "mfma.hip", "mfma_q8_0_bf16.hip",
            "mfma_q8_0_f16.hip", "mfma_q4_0_bf16.hip", "mfma_q4_0_f16.hip", "mfma_q6_s_bf16.hip", "mfma_q6_s_f16.hip", "mfma_rows.hip",
            "mfma_rows_q8_0.hip", "mfma_rows_q4_0.hip", "mfma_q6.hip", "gemv_q6.hip", "mfma_i8.hip",
-           "attention_api.cpp", "kv_extend.hip", "rope.hip", "attention.hip"]
+           "attention_api.cpp", "kv_extend.hip", "rope.hip", "attention.hip",
+           "attention_bf16.hip", "attention_f16.hip"]
 COMMON = ["-O3", "-std=c++17", "-fPIC", f"--offload-arch={ARCH}", "-I", INCLUDE, "-I", CSRC,
           "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
           "-fhip-fp32-correctly-rounded-divide-sqrt", "-fno-gpu-flush-denormals-to-zero",

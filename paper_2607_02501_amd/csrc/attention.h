@@ -16,4 +16,29 @@ hipError_t launch_rope_append(const eb_rope_append_op &o, hipStream_t s);
 size_t attention_ws_bytes(const eb_attention_op &o);
 hipError_t launch_attention(const eb_attention_op &o, void *ws, hipStream_t s);
 
+// What the attention kernels take beside the op itself.
+struct AttnArgs {
+  eb_attention_op o;
+  float *ws;           // sums of splits
+  int64_t head_rows;   // cache rows of a page: heads * page
+  int32_t page_shift;
+  int32_t kv_max;      // keys of a table row
+  int32_t group;       // query heads per key/value head
+  int32_t tile_rows;   // 128: the tile kernel, 32: the stream kernel
+  int32_t unit;        // keys that splits are counted in
+  int32_t min_units;   // of a split
+  int32_t target;      // items of a key/value head that splits may add; 0: no splits
+  int32_t part_rows;   // rows of a tile that a split may have sums of
+  uint32_t items;      // of a key/value head, at most
+  uint32_t grid;       // items of all heads
+  uint32_t grid_wgs;   // workgroups: grid rounded up to the XCDs
+  uint32_t flip;       // sign bits of a pair of queries where the scale is negative
+  float scale2;        // 2^(scale2 s) without a cap; 2^(scale2 s) = e^(2 scale s / cap) with one
+  float cap2;          // cap * log2 e, 0 without a cap
+};
+
+// The kernels of one cache type (attention_bf16.hip, attention_f16.hip).
+template <int T>
+hipError_t attn_launch(const AttnArgs &a, hipStream_t s);
+
 }  // namespace eb

@@ -12,6 +12,7 @@ namespace {
 
 constexpr int64_t kMaxRows = int64_t(1) << 24;
 constexpr int64_t kMaxInt = 0x7fffffff;
+constexpr int64_t kMaxKeys = int64_t(1) << 30;  // of a sequence: keys count in 32 bits
 
 bool aligned(const void *p, uintptr_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
 
@@ -59,7 +60,7 @@ int64_t row_bytes(int64_t rows, int64_t stride, int64_t width, int64_t size) {
 eb_status check_extend(const eb_kv_extend_op &o) {
   if (o.batch < 1 || o.batch > kMaxBatch || o.rows < 0 || o.rows > kMaxRows || !pow2_page(o.page) ||
       o.pages < 1 || (int64_t)o.pages * o.page > kMaxInt || o.table_stride < 1 ||
-      (int64_t)o.table_stride * o.page > kMaxInt || o.free_capacity < 0)
+      (int64_t)o.table_stride * o.page > kMaxKeys || o.free_capacity < 0)
     return EB_ERR_INVALID;
   if (!o.cached || !o.added || !o.table || !o.n_free || !o.n_free_out || !o.q_start || !o.kv_len ||
       !o.short_rows || (o.free_capacity > 0 && !o.free_pages) || (o.rows > 0 && (!o.slots || !o.positions)))
@@ -129,7 +130,7 @@ eb_status check_attention(const eb_attention_op &o) {
   if (o.rows < 0 || o.rows > kMaxRows || o.batch < 1 || o.batch > kMaxBatch || o.q_heads < 1 ||
       o.q_heads > 4096 || o.q_heads % o.cache.heads != 0 || o.q_stride < width || o.out_stride < width ||
       o.q_stride > kMaxInt || o.out_stride > kMaxInt || o.table_stride < 1 ||
-      (int64_t)o.table_stride * o.cache.page > kMaxInt || o.max_new < 1 || o.max_kv < 1 || o.window < 0 ||
+      (int64_t)o.table_stride * o.cache.page > kMaxKeys || o.max_new < 1 || o.max_kv < 1 || o.window < 0 ||
       (o.mask != EB_MASK_CAUSAL && o.mask != EB_MASK_FULL))
     return EB_ERR_INVALID;
   if (!std::isfinite(o.scale) || !(std::isfinite(o.softcap) && o.softcap >= 0.0f)) return EB_ERR_INVALID;

@@ -1,0 +1,917 @@
+// attention_tile.h -- attention of new tokens over a paged cache on the matrix
+// cores: the kernels behind eb_attention (include/eb_attention.h), instantiated
+// for each cache type in its own translation unit.
+//
+// Rows.  The query heads of one key/value head and the new tokens of a sequence
+// form its rows: row R is token R / group, head R % group of the group.  A
+// workgroup of four waves takes a tile of rows of one sequence and key/value head
+// and a range of its keys; a wave takes 32 rows.
+//
+// Products.  S^T = K Q^T, so that a lane holds the scores of one row (column
+// lane % 32 of the 32 x 32 result) and softmax statistics need no more than one
+// exchange with lane ^ 32; then O^T += V^T P^T, whose P^T operand is the scores'
+// own registers: result register i of lane half h is key 8 (i / 4) + 4 h + i % 4,
+// and the order of the 16 keys of a product's contraction is free, so V^T is
+// read in that order (transposing LDS reads, 4 keys of one element per lane) and
+// no score changes lanes.
+//
+// Softmax.  One pass, with a running maximum m and sum l per row in fp32; p =
+// 2^((s - m) c).  m is raised, and O and l rescaled, only when a row's maximum
+// has grown by more than a factor 2^8 in p: p then stays below 2^8, and most
+// tiles skip the rescale.  p enters the product rounded to the cache's type (its
+// sum l takes p itself).
+//
+// Masks.  The keys a row sees are one interval; a tile that lies inside every
+// row's interval skips the comparisons.  Keys past the sequence's end and on
+// missing pages are read as zeros (buffer bounds), so what the cache holds there
+// cannot reach a sum.  A key that only some rows of the tile see enters the
+// product of the others with p = 0, which hides any value but infinities and
+// NaN: a row whose result is not finite is computed again, key by key
+// (row_again).
+#ifndef EB_ATTENTION_TILE_H
+#define EB_ATTENTION_TILE_H
+
+#include <hip/hip_runtime.h>
+
+#include "attention.h"
+#include "epilogue.h"
+#include "mfma_common.h"
+
+namespace eb {
+namespace {
+
+typedef short s16x4_t __attribute__((ext_vector_type(4)));
+
+// ---------------------------------------------------------------------------
+// which rows and keys a workgroup takes
+// ---------------------------------------------------------------------------
+
+struct Item {
+  int32_t b = -1;        // sequence, -1: none
+  int32_t tile = 0;      // row tile of the sequence
+  int32_t split = 0, splits = 1;
+  int32_t q0 = 0, n = 0;  // first row of q, new tokens to compute
+  int32_t p0 = 0;        // place of the first new token
+  int32_t kv = 0;
+};
+
+struct Seq {
+  int32_t q0, n, p0, kv, tiles, units;
+};
+
+__device__ inline Seq seq_of(const AttnArgs &a, int32_t b) {
+  const eb_attention_op &o = a.o;
+  Seq s;
+  const int32_t r0 = min(max(o.q_start[b], 0), o.rows), r1 = min(max(o.q_start[b + 1], r0), o.rows);
+  s.kv = min(max(o.kv_len[b], 0), a.kv_max);
+  s.q0 = r0;
+  s.p0 = s.kv - (r1 - r0);
+  s.n = min(r1 - r0, o.max_new);
+  s.tiles = (int32_t)(((int64_t)s.n * a.group + a.tile_rows - 1) / a.tile_rows);
+  // units of keys that a tile may see
+  int64_t see = s.kv;
+  if (o.window > 0 && o.mask != EB_MASK_FULL && !o.prefix) see = min(see, (int64_t)o.window + a.tile_rows);
+  s.units = (int32_t)((see + a.unit - 1) / a.unit);
+  return s;
+}
+
+__device__ inline int64_t wave_sum(int64_t v) {
+#pragma unroll
+  for (int d = 32; d >= 1; d >>= 1) v += __shfl_xor(v, d);
+  return v;
+}
+
+// Item number `at` of a key/value head: the sequences' row tiles in order, each
+// `splits` times.  A sequence's tiles are split so that a split is at least
+// a.min_units units long and the splits of all sequences together about
+// a.target items (a longer sequence gets more); every wave of every workgroup
+// finds the same numbers from the lengths.
+__device__ inline Item find_item(const AttnArgs &a, int64_t at) {
+  const eb_attention_op &o = a.o;
+  const int lane = threadIdx.x & 63;
+  Item it;
+  Seq s;
+  int32_t splits = 1;
+  int64_t rest = at;
+  auto per_split = [&](int64_t units) {
+    const int64_t share = (units + a.target - 1) / a.target;
+    return share > a.min_units ? share : (int64_t)a.min_units;
+  };
+  auto splits_of = [&](const Seq &q, int64_t per) {
+    return a.target > 0 && q.units > 0 ? (int32_t)((q.units + per - 1) / per) : 1;
+  };
+  if (o.batch == 1) {
+    s = seq_of(a, 0);
+    if (a.target > 0) splits = splits_of(s, per_split((int64_t)s.tiles * s.units));
+    if (at >= (int64_t)s.tiles * splits) return it;
+    it.b = 0;
+  } else {
+    int64_t per = 1;
+    if (a.target > 0) {
+      int64_t units = 0;
+      for (int32_t b0 = 0; b0 < o.batch; b0 += 64) {
+        const int32_t b = b0 + lane;
+        if (b < o.batch) {
+          const Seq q = seq_of(a, b);
+          units += (int64_t)q.tiles * q.units;
+        }
+      }
+      per = per_split(wave_sum(units));
+    }
+    for (int32_t b0 = 0; b0 < o.batch; b0 += 64) {
+      const int32_t b = b0 + lane;
+      int64_t items = 0;
+      if (b < o.batch) {
+        s = seq_of(a, b);
+        splits = splits_of(s, per);
+        items = (int64_t)s.tiles * splits;
+      }
+      int64_t sum = items;
+#pragma unroll
+      for (int d = 1; d < 64; d <<= 1) {
+        const int64_t u = __shfl_up(sum, d);
+        if (lane >= d) sum += u;
+      }
+      const uint64_t past = __ballot(sum > rest);
+      if (past) {
+        const int src = __builtin_ctzll(past);
+        rest -= __shfl(sum - items, src);
+        s.q0 = __shfl(s.q0, src);
+        s.n = __shfl(s.n, src);
+        s.p0 = __shfl(s.p0, src);
+        s.kv = __shfl(s.kv, src);
+        splits = __shfl(splits, src);
+        it.b = b0 + src;
+        break;
+      }
+      rest -= __shfl(sum, 63);
+    }
+    if (it.b < 0) return it;
+  }
+  auto uni = [](int32_t v) { return __builtin_amdgcn_readfirstlane(v); };
+  it.b = uni(it.b);
+  it.splits = uni(splits);
+  it.tile = uni((int32_t)(rest / it.splits));
+  it.split = uni((int32_t)(rest % it.splits));
+  it.q0 = uni(s.q0);
+  it.n = uni(s.n);
+  it.p0 = uni(s.p0);
+  it.kv = uni(s.kv);
+  return it;
+}
+
+// The keys lo <= j < hi that the token at place p sees.
+__device__ inline void interval(const AttnArgs &a, int32_t p, int32_t kv, int32_t prefix, int32_t &lo,
+                                int32_t &hi) {
+  hi = a.o.mask == EB_MASK_FULL ? kv : min(kv, max(p + 1, prefix));
+  lo = a.o.window > 0 && p >= a.o.window ? p - a.o.window + 1 : 0;
+}
+
+// ---------------------------------------------------------------------------
+// pages and copies to LDS
+// ---------------------------------------------------------------------------
+
+// Page numbers of 64 consecutive table entries, one per lane, and of the 64
+// after them, requested while these are used: at least 1024 keys of each.
+struct Pages {
+  const int32_t *table;  // of the sequence
+  int32_t count;         // entries that hold its keys
+  int32_t pages;         // valid page numbers are below
+  int32_t first;         // entry of lane 0
+  int32_t now, next;
+
+  __device__ int32_t load(int32_t at) const {
+    const int32_t i = at + (int32_t)(threadIdx.x & 63);
+    const int32_t id = i < count ? table[i] : -1;
+    return id < pages ? id : -1;
+  }
+  __device__ void begin(int32_t at) {
+    first = at;
+    now = load(at);
+    next = load(at + 64);
+  }
+  // Makes entry `at` (which never decreases) one of `now`'s.
+  __device__ void reach(int32_t at) {
+    while (at - first >= 64) {
+      first += 64;
+      now = next;
+      next = load(first + 64);
+    }
+  }
+  __device__ int32_t id(int32_t at) const { return __builtin_amdgcn_readlane(now, at - first); }
+};
+
+// Copies of a cache tile: ROWS keys of D elements from key k0 on go to LDS rows of
+// D / 8 chunks of 16 bytes, by NW waves of which this is number wv.  Chunk c of
+// row r is stored at c ^ swizzle: for keys (read as 8 chunks of one column by 8
+// rows) r % 8, for values (read as 4 rows by 2 chunks) 2 (r % 8), or 2 (r % 4) in
+// rows of 8 chunks, so that a read's lanes fall on different banks.
+template <int D>
+__device__ inline uint32_t k_swizzle(uint32_t r) { return r & 7; }
+template <int D>
+__device__ inline uint32_t v_swizzle(uint32_t r) { return (r & (D == 64 ? 3 : 7)) << 1; }
+
+template <int D, int ROWS, int NW, bool V>
+struct Copy {
+  static constexpr int kChunks = D / 8;
+  static constexpr int kRows = 64 / kChunks;  // of one wave's copy
+  static constexpr int kCopies = ROWS / kRows / NW;
+
+  __device__ static void issue(const uint8_t *cache, int64_t head_rows, int64_t head, int page_shift,
+                               const Pages &pg, int32_t k0, int32_t kv, uint32_t lds, int wv) {
+    const int lane = threadIdx.x & 63;
+    const uint32_t lr = lane / kChunks, lc = lane % kChunks;
+#pragma unroll
+    for (int n = 0; n < kCopies; ++n) {
+      const int row0 = (n * NW + wv) * kRows;  // same in all lanes
+      const uint32_t r = row0 + lr;
+      const uint32_t chunk = lc ^ (V ? v_swizzle<D>(r) : k_swizzle<D>(r));
+      const int32_t key = __builtin_amdgcn_readfirstlane(k0 + row0);
+      const int32_t id = pg.id(key >> page_shift);
+      const int32_t in_page = key & ((1 << page_shift) - 1);
+      // rows past the end, and those of a missing page, are zeros
+      const int32_t rows = id < 0 ? 0 : min(max(kv - key, 0), kRows);
+      const int64_t at = ((id < 0 ? 0 : (int64_t)id) * head_rows + head + in_page) * (D * 2);
+      i32x4_t r4 = rsrc4(cache + at, (uint32_t)rows * (D * 2));
+#pragma unroll
+      for (int i = 0; i < 3; ++i) r4[i] = __builtin_amdgcn_readfirstlane(r4[i]);
+      copy_lds(r4, lr * (D * 2) + chunk * 16, lds + (uint32_t)(n * NW + wv) * 1024);
+    }
+  }
+};
+
+template <int N>
+__device__ inline void wait_vm() {
+  __builtin_amdgcn_sched_barrier(0);
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(N) : "memory");
+  __builtin_amdgcn_sched_barrier(0);
+}
+
+__device__ inline uint32_t lds_addr(const void *p) {
+  return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void *)p;
+}
+
+// ---------------------------------------------------------------------------
+// one wave's 32 rows
+// ---------------------------------------------------------------------------
+
+template <int T, int D, int BK, bool CAP>
+struct Wave {
+  static constexpr int kSteps = D / 16;   // of a score's contraction
+  static constexpr int kBlocks = D / 32;  // of output elements
+  static constexpr int kTiles = BK / 32;  // of scores
+
+  uint4 q[kSteps];
+  f32x16_t o[kBlocks];
+  float m, l;
+  int32_t lo, hi;        // keys that this lane's row sees (a lane without a row: all)
+  int32_t all_lo, all_hi;  // keys that every row of the wave sees
+  int32_t any_lo, any_hi;  // and that some row sees
+  bool masked;           // a tile was compared
+
+  __device__ void begin() {
+#pragma unroll
+    for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) o[b][i] = 0.f;
+    m = -INFINITY;
+    l = 0.f;
+    masked = false;
+  }
+
+  // A row's value in lane l and in lane l ^ 32, in both lanes.  The exchange swaps
+  // halves of two registers; of one register, given twice, it makes nothing useful,
+  // and the compiler would give one where both are the same value.
+  __device__ static float2 both(float v) {
+    uint32_t x = __builtin_bit_cast(uint32_t, v), y = x;
+    asm("" : "+v"(y));
+    const auto r = __builtin_amdgcn_permlane32_swap(x, y, false, false);
+    return make_float2(__builtin_bit_cast(float, (uint32_t)r[0]), __builtin_bit_cast(float, (uint32_t)r[1]));
+  }
+  __device__ static float row_max(float v) {
+    const float2 r = both(v);
+    return fmaxf(r.x, r.y);
+  }
+  __device__ static float row_sum(float v) {
+    const float2 r = both(v);
+    return r.x + r.y;
+  }
+
+  // Scores of BK keys in LDS.
+  __device__ void scores(f32x16_t (&s)[kTiles], const uint8_t *k) const {
+    const uint32_t lane = threadIdx.x & 63, row = lane & 31, half = lane >> 5;
+    const uint8_t *const base = k + row * (D * 2);
+    const uint32_t x = half ^ k_swizzle<D>(row);
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[t][i] = 0.f;
+#pragma unroll
+    for (int c = 0; c < kSteps; ++c)
+#pragma unroll
+      for (int t = 0; t < kTiles; ++t) {
+        const uint4 a = *reinterpret_cast<const uint4 *>(base + t * (32 * D * 2) + (((2 * c) & ~7) << 4) +
+                                                         ((((2 * c) & 7) ^ x) << 4));
+        s[t] = mfma32<T>(a, q[c], s[t]);
+      }
+  }
+
+  // From scores to p, with the maximum and sum of each row; p in pairs.
+  __device__ void softmax(const AttnArgs &a, f32x16_t (&s)[kTiles], uint32_t (&p)[kTiles][8], int32_t k0,
+                          uint32_t missing) {
+    const int half = (threadIdx.x & 63) >> 5;
+    const float c = CAP ? 1.f : a.scale2;
+    if (CAP) {
+#pragma unroll
+      for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const float e = __builtin_amdgcn_exp2f(s[t][i] * a.scale2);
+          s[t][i] = __builtin_fmaf(-2.f * a.cap2, __builtin_amdgcn_rcpf(1.f + e), a.cap2);
+        }
+    }
+    if (k0 < all_lo || k0 + BK > all_hi || missing) {
+      masked = true;
+#pragma unroll
+      for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const int32_t key = k0 + 32 * t + 8 * (i / 4) + 4 * half + i % 4;
+          const bool see = key >= lo && key < hi && !(missing >> (2 * t + i / 8) & 1);
+          s[t][i] = see ? s[t][i] : -INFINITY;
+        }
+    }
+    float top = s[0][0];
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) top = fmaxf(top, s[t][i]);
+    top = row_max(top);
+    if (__ballot((top - m) * c > 8.f)) {
+      const float to = fmaxf(m, top);
+      const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m - to) * c);
+      m = to;
+      l *= f;
+#pragma unroll
+      for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[b][i] *= f;
+    }
+    const float base = m == -INFINITY ? 0.f : -m * c;
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+      for (int i = 0; i < 16; i += 2) {
+        const float u = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][i], c, base));
+        const float v = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][i + 1], c, base));
+        l += u + v;
+        p[t][i / 2] = pack2<T>(u, v);
+      }
+  }
+
+  // O^T += V^T P^T over BK keys in LDS.
+  __device__ void values(const uint32_t (&p)[kTiles][8], const uint8_t *v) {
+    const uint32_t lane = threadIdx.x & 63, half = lane >> 5;
+    const uint32_t row = 4 * half + (lane & 15) / 4, quad = lane & 3;
+    const uint32_t x = (2 * ((lane >> 4) & 1) + quad / 2) ^ v_swizzle<D>(row);
+    const uint32_t base = lds_addr(v) + row * (D * 2) + (quad & 1) * 8;
+#pragma unroll
+    for (int c = 0; c < 2 * kTiles; ++c) {
+      const uint32_t *w = &p[c / 2][4 * (c % 2)];
+      const uint4 pb = make_uint4(w[0], w[1], w[2], w[3]);
+#pragma unroll
+      for (int b = 0; b < kBlocks; ++b) {
+        const uint32_t at = base + (16 * c) * (D * 2) + (((4 * b) & ~15) << 4) + ((((4 * b) & 15) ^ x) << 4);
+        auto read = [](uint32_t addr) {
+          return __builtin_bit_cast(
+              uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                         (__attribute__((address_space(3))) s16x4_t *)(uintptr_t)addr));
+        };
+        const uint2 v0 = read(at), v1 = read(at + 8 * (D * 2));
+        o[b] = mfma32<T>(make_uint4(v0.x, v0.y, v1.x, v1.y), pb, o[b]);
+      }
+    }
+  }
+
+  __device__ bool finite() const {
+    float z = l * 0.f;
+#pragma unroll
+    for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) z = __builtin_fmaf(o[b][i], 0.f, z);
+    return z == 0.f;
+  }
+};
+
+// Loads the queries of a lane's row as the operand of scores(): elements 16 c +
+// 8 half .. + 7 of step c; with a negative scale, negated (exactly).
+template <int D>
+__device__ inline void load_query(uint4 (&q)[D / 16], const uint16_t *row, uint32_t flip) {
+  const int half = (threadIdx.x & 63) >> 5;
+#pragma unroll
+  for (int c = 0; c < D / 16; ++c) {
+    q[c] = row ? *reinterpret_cast<const uint4 *>(row + 16 * c + 8 * half) : make_uint4(0, 0, 0, 0);
+    q[c].x ^= flip;
+    q[c].y ^= flip;
+    q[c].z ^= flip;
+    q[c].w ^= flip;
+  }
+}
+
+// ---------------------------------------------------------------------------
+// one row by one wave, key by key: exact about what the row does not see
+// ---------------------------------------------------------------------------
+
+template <int T, int D>
+struct Row {
+  static constexpr int kElems = D / 64;  // of a lane: lane * kElems + e
+  float m, l, acc[kElems];
+};
+
+template <int T, int D, bool CAP>
+__device__ inline void row_again(const AttnArgs &a, const uint16_t *qrow, int64_t head,
+                                                    const int32_t *table, int32_t count, int32_t lo,
+                                                    int32_t hi, Row<T, D> *out) {
+  constexpr int E = D / 64;
+  const eb_attention_op &o = a.o;
+  const int lane = threadIdx.x & 63;
+  float qe[E], acc[E] = {};
+#pragma unroll
+  for (int e = 0; e < E; ++e) qe[e] = from_y16(qrow[lane * E + e] ^ (uint16_t)a.flip, T);
+  float m = -INFINITY, l = 0.f;
+  const float c = CAP ? 1.f : a.scale2;
+  for (int32_t j0 = lo; j0 < hi; j0 += 64) {
+    const int32_t j = j0 + lane, at = j >> a.page_shift;
+    int32_t id = j < hi && at < count ? table[at] : -1;
+    if (id >= o.cache.pages) id = -1;
+    const int64_t row = (max(id, 0) * a.head_rows + head + (j & (o.cache.page - 1))) * D;
+    float t = -INFINITY;
+    {
+      const uint4 *k = reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(o.cache.k) + row);
+      float s = 0.f;
+      for (int ch = 0; ch < D / 8; ++ch) {
+        uint32_t w[4] = {0, 0, 0, 0};
+        if (id >= 0) {
+          const uint4 u = k[ch];
+          w[0] = u.x, w[1] = u.y, w[2] = u.z, w[3] = u.w;
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const int e = 8 * ch + i;
+          const float x = __shfl(qe[i % E], e / E);
+          s = __builtin_fmaf(from_y16((uint16_t)(w[i / 2] >> (16 * (i & 1))), T), x, s);
+        }
+      }
+      if (CAP) {
+        const float e = __builtin_amdgcn_exp2f(s * a.scale2);
+        s = __builtin_fmaf(-2.f * a.cap2, __builtin_amdgcn_rcpf(1.f + e), a.cap2);
+      }
+      if (id >= 0) t = s;
+    }
+    float top = t;
+#pragma unroll
+    for (int d = 32; d >= 1; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
+    const float to = fmaxf(m, top), base = to == -INFINITY ? 0.f : to;
+    const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m - base) * c);
+    const float w = id >= 0 ? __builtin_amdgcn_exp2f((t - base) * c) : 0.f;
+    m = to;
+    float sum = w;
+#pragma unroll
+    for (int d = 32; d >= 1; d >>= 1) sum += __shfl_xor(sum, d);
+    l = l * f + sum;
+#pragma unroll
+    for (int e = 0; e < E; ++e) acc[e] *= f;
+    for (uint64_t left = __ballot(id >= 0); left; left &= left - 1) {
+      const int src = __builtin_ctzll(left);
+      const float wk = __shfl(w, src);
+      const uint16_t *v = static_cast<const uint16_t *>(o.cache.v) + __shfl(row, src) + lane * E;
+#pragma unroll
+      for (int e = 0; e < E; ++e) acc[e] = __builtin_fmaf(wk, from_y16(v[e], T), acc[e]);
+    }
+  }
+  out->m = m;
+  out->l = l;
+#pragma unroll
+  for (int e = 0; e < E; ++e) out->acc[e] = acc[e];
+}
+
+// ---------------------------------------------------------------------------
+// kernels
+// ---------------------------------------------------------------------------
+
+// Sums of a split, for rows [item][row of the tile]: D values, then m c and l.
+__device__ inline float *partial(const AttnArgs &a, int64_t item, int32_t row, int d) {
+  return a.ws + (item * a.part_rows + row) * (d + 2);
+}
+
+// This workgroup's item and key/value head.  Neighbouring workgroups go to the 8
+// XCDs in turn; each XCD gets a contiguous run of (head, item) so that tiles of
+// one sequence and head, which read the same keys, share its L2.
+__device__ inline void locate(const AttnArgs &a, int32_t &head, int64_t &at) {
+  const uint32_t per = (a.grid + kXcds - 1) / kXcds;
+  const uint32_t id = (blockIdx.x % kXcds) * per + blockIdx.x / kXcds;
+  head = (int32_t)(id / a.items);
+  at = id % a.items;
+}
+
+// The row of q / out that row `r` of an item's tile is, or -1.
+__device__ inline int64_t row_of(const AttnArgs &a, const Item &it, int32_t r, int32_t kh, int32_t &tok,
+                                 int32_t &head) {
+  const int64_t R = (int64_t)it.tile * a.tile_rows + r;
+  tok = (int32_t)(R / a.group);
+  head = kh * a.group + (int32_t)(R % a.group);
+  return tok < it.n ? (int64_t)it.q0 + tok : -1;
+}
+
+// Intervals of a wave's rows: each lane's own, and bounds over the lanes.
+template <class W>
+__device__ inline void intervals(const AttnArgs &a, const Item &it, int32_t tok, bool live, W &w) {
+  const int32_t prefix = a.o.prefix ? a.o.prefix[it.b] : 0;
+  interval(a, it.p0 + tok, it.kv, prefix, w.lo, w.hi);
+  if (!live) w.lo = 0, w.hi = 0x7fffffff;
+  int32_t al = live ? w.lo : 0, ah = live ? w.hi : 0x7fffffff, yl = live ? w.lo : 0x7fffffff,
+          yh = live ? w.hi : 0;
+#pragma unroll
+  for (int d = 16; d >= 1; d >>= 1) {
+    al = max(al, __shfl_xor(al, d));
+    ah = min(ah, __shfl_xor(ah, d));
+    yl = min(yl, __shfl_xor(yl, d));
+    yh = max(yh, __shfl_xor(yh, d));
+  }
+  w.all_lo = __builtin_amdgcn_readfirstlane(al);
+  w.all_hi = __builtin_amdgcn_readfirstlane(ah);
+  w.any_lo = __builtin_amdgcn_readfirstlane(yl);
+  w.any_hi = __builtin_amdgcn_readfirstlane(yh);
+}
+
+// Tiles of BK keys [t0, t1) of a split of [lo, hi).
+template <int BK>
+__device__ inline void split_range(const Item &it, int32_t lo, int32_t hi, int32_t &t0, int32_t &t1) {
+  const int32_t a = lo / BK, b = hi > lo ? (hi + BK - 1) / BK : a;
+  t0 = a + (int32_t)((int64_t)(b - a) * it.split / it.splits);
+  t1 = a + (int32_t)((int64_t)(b - a) * (it.split + 1) / it.splits);
+}
+
+// Bit s is set where the 16 keys from k0 + 16 s on are on a missing page.
+template <int BK>
+__device__ inline uint32_t missing_of(const Pages &pg, int32_t k0, int32_t kv, int page_shift) {
+  uint32_t bits = 0;
+#pragma unroll
+  for (int s = 0; s < BK / 16; ++s)
+    if (k0 + 16 * s < kv && pg.id((k0 + 16 * s) >> page_shift) < 0) bits |= 1u << s;
+  return bits;
+}
+
+// Many rows: 128 of a tile, 32 to each wave, all waves over the same keys, which
+// are copied to LDS one tile ahead (one barrier a tile).
+template <int T, int D, int BK, bool CAP>
+__global__ void __launch_bounds__(256, D == 256 ? 1 : 2) attn_tile_kernel(AttnArgs a) {
+  constexpr int kTile = BK * D * 2;  // bytes of a tile of keys or values
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[4 * kTile];
+  const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  int32_t kh;
+  int64_t at;
+  locate(a, kh, at);
+  if (kh >= a.o.cache.heads) return;
+  const Item it = find_item(a, at);
+  if (it.b < 0) return;
+
+  Wave<T, D, BK, CAP> w;
+  int32_t tok, head;
+  const int64_t row = row_of(a, it, 32 * wv + (lane & 31), kh, tok, head);
+  const bool live = row >= 0;
+  const uint16_t *qrow =
+      live ? static_cast<const uint16_t *>(a.o.q) + row * a.o.q_stride + (int64_t)head * D : nullptr;
+  load_query<D>(w.q, qrow, a.flip);
+  intervals(a, it, tok, live, w);
+  w.begin();
+
+  // keys that any row of the workgroup sees: its first and last token bound them
+  int32_t lo, hi, t0, t1;
+  {
+    const int32_t first = (int32_t)((int64_t)it.tile * 128 / a.group);
+    const int32_t last = min((int32_t)(((int64_t)it.tile * 128 + 127) / a.group), it.n - 1);
+    const int32_t prefix = a.o.prefix ? a.o.prefix[it.b] : 0;
+    int32_t x;
+    interval(a, it.p0 + first, it.kv, prefix, lo, x);
+    interval(a, it.p0 + last, it.kv, prefix, x, hi);
+  }
+  split_range<BK>(it, lo, hi, t0, t1);
+  Pages pg;
+  pg.table = a.o.table + (int64_t)it.b * a.o.table_stride;
+  pg.count = (it.kv + a.o.cache.page - 1) >> a.page_shift;
+  pg.pages = a.o.cache.pages;
+  const int64_t hr = a.head_rows, ho = (int64_t)kh << a.page_shift;
+  const uint32_t base = lds_addr(lds);
+  auto request = [&](int32_t t) {
+    const int32_t k0 = t * BK;
+    const uint32_t to = base + (uint32_t)(t & 1) * (2 * kTile);
+    pg.reach(k0 >> a.page_shift);
+    Copy<D, BK, 4, false>::issue(static_cast<const uint8_t *>(a.o.cache.k), hr, ho, a.page_shift, pg, k0,
+                                 it.kv, to, wv);
+    Copy<D, BK, 4, true>::issue(static_cast<const uint8_t *>(a.o.cache.v), hr, ho, a.page_shift, pg, k0,
+                                it.kv, to + kTile, wv);
+    return missing_of<BK>(pg, k0, it.kv, a.page_shift);
+  };
+  uint32_t gone = 0;
+  if (t0 < t1) {
+    pg.begin((t0 * BK) >> a.page_shift);
+    gone = request(t0);
+  }
+  for (int32_t t = t0; t < t1; ++t) {
+    // tile t is in LDS, and every wave has done with the tile before it
+    wait_vm_barrier<0>();
+    const uint32_t missing = gone;
+    if (t + 1 < t1) gone = request(t + 1);
+    const int32_t k0 = t * BK;
+    if (k0 < w.any_hi && k0 + BK > w.any_lo) {
+      const uint8_t *k = lds + (t & 1) * (2 * kTile);
+      f32x16_t s[BK / 32];
+      uint32_t p[BK / 32][8];
+      w.scores(s, k);
+      w.softmax(a, s, p, k0, missing);
+      w.values(p, k + kTile);
+    }
+  }
+
+  w.l = Wave<T, D, BK, CAP>::row_sum(w.l);
+  const bool split = it.splits > 1;
+  const float c = CAP ? 1.f : a.scale2;
+  const int64_t item = (int64_t)kh * a.items + at;
+  const int half = lane >> 5;
+  if (live) {
+    if (split) {
+      float *dst = partial(a, item, 32 * wv + (lane & 31), D);
+#pragma unroll
+      for (int b = 0; b < D / 32; ++b)
+#pragma unroll
+        for (int i = 0; i < 16; i += 2)
+          *reinterpret_cast<float2 *>(dst + 32 * b + 8 * (i / 4) + 4 * half + i % 4) =
+              make_float2(w.o[b][i], w.o[b][i + 1]);
+      if (half == 0) *reinterpret_cast<float2 *>(dst + D) = make_float2(w.m * c, w.l);
+    } else {
+      uint16_t *dst = static_cast<uint16_t *>(a.o.out) + row * a.o.out_stride + (int64_t)head * D;
+      const float inv = w.l != 0.f ? 1.f / w.l : 0.f;
+#pragma unroll
+      for (int b = 0; b < D / 32; ++b)
+#pragma unroll
+        for (int i = 0; i < 16; i += 4)
+          *reinterpret_cast<uint2 *>(dst + 32 * b + 8 * (i / 4) + 4 * half) =
+              make_uint2(pack2<T>(w.o[b][i] * inv, w.o[b][i + 1] * inv),
+                         pack2<T>(w.o[b][i + 2] * inv, w.o[b][i + 3] * inv));
+    }
+  }
+  // rows whose sums took up an infinity or NaN where some key was hidden
+  uint64_t again = __ballot(live && w.masked && !w.finite());
+  again = (again | again >> 32) & 0xffffffffu;
+  while (again) {
+    const int src = __builtin_ctzll(again);
+    again &= again - 1;
+    const int32_t klo = max(__builtin_amdgcn_readlane(w.lo, src), t0 * BK);
+    const int32_t khi = min(__builtin_amdgcn_readlane(w.hi, src), t1 * BK);
+    int32_t tk, hd;
+    const int64_t rw = row_of(a, it, 32 * wv + src, kh, tk, hd);
+    Row<T, D> r;
+    row_again<T, D, CAP>(a, static_cast<const uint16_t *>(a.o.q) + rw * a.o.q_stride + (int64_t)hd * D, ho,
+                         pg.table, pg.count, klo, khi, &r);
+    constexpr int E = D / 64;
+    if (split) {
+      float *dst = partial(a, item, 32 * wv + src, D);
+#pragma unroll
+      for (int e = 0; e < E; ++e) dst[lane * E + e] = r.acc[e];
+      if (lane == 0) dst[D] = r.m * c, dst[D + 1] = r.l;
+    } else {
+      uint16_t *dst = static_cast<uint16_t *>(a.o.out) + rw * a.o.out_stride + (int64_t)hd * D;
+      const float inv = r.l != 0.f ? 1.f / r.l : 0.f;
+#pragma unroll
+      for (int e = 0; e < E; ++e) dst[lane * E + e] = to_y16(r.acc[e] * inv, T);
+    }
+  }
+}
+
+// Few rows: up to 32, the same for all waves, which take the tiles of 32 keys in
+// turn.  A wave copies its own tiles to its own part of LDS, keys while it works
+// on values and values while it works on keys, and waits for no other wave; the
+// four waves' sums are joined in LDS at the end.
+template <int T, int D, bool CAP>
+__global__ void __launch_bounds__(256, 1) attn_stream_kernel(AttnArgs a) {
+  constexpr int BK = 32, kTile = BK * D * 2;
+  using K = Copy<D, BK, 1, false>;
+  using V = Copy<D, BK, 1, true>;
+  static_assert(2 * kTile == 32 * D * 4, "a wave's tiles and its sums take the same room");
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[4 * 2 * kTile];
+  __shared__ float ml[2][4][32];
+  __shared__ uint32_t again;
+  const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  int32_t kh;
+  int64_t at;
+  locate(a, kh, at);
+  if (kh >= a.o.cache.heads) return;
+  const Item it = find_item(a, at);
+  if (it.b < 0) return;
+
+  Wave<T, D, BK, CAP> w;
+  int32_t tok, head;
+  const int64_t row = row_of(a, it, lane & 31, kh, tok, head);
+  const bool live = row >= 0;
+  Pages pg;
+  pg.table = a.o.table + (int64_t)it.b * a.o.table_stride;
+  pg.count = (it.kv + a.o.cache.page - 1) >> a.page_shift;
+  pg.pages = a.o.cache.pages;
+  intervals(a, it, tok, live, w);
+  int32_t t0, t1;
+  split_range<BK>(it, w.any_lo, w.any_hi, t0, t1);
+  const int64_t hr = a.head_rows, ho = (int64_t)kh << a.page_shift;
+  uint8_t *const mine = lds + wv * (2 * kTile);
+  const uint32_t to = lds_addr(mine);
+  auto keys = [&](int32_t t) {  // past t1: nothing to read, but the copies count
+    const int32_t k0 = t * BK;
+    if (t < t1) pg.reach(k0 >> a.page_shift);
+    K::issue(static_cast<const uint8_t *>(a.o.cache.k), hr, ho, a.page_shift, pg,
+             t < t1 ? k0 : pg.first << a.page_shift, t < t1 ? it.kv : 0, to, 0);
+  };
+  auto values = [&](int32_t t) {
+    const int32_t k0 = t * BK;
+    V::issue(static_cast<const uint8_t *>(a.o.cache.v), hr, ho, a.page_shift, pg,
+             t < t1 ? k0 : pg.first << a.page_shift, t < t1 ? it.kv : 0, to + kTile, 0);
+  };
+  const int32_t begin = t0 + wv;
+  if (begin < t1) {
+    pg.begin((begin * BK) >> a.page_shift);
+    keys(begin);
+    values(begin);
+  }
+  load_query<D>(w.q, live ? static_cast<const uint16_t *>(a.o.q) + row * a.o.q_stride + (int64_t)head * D
+                          : nullptr, a.flip);
+  w.begin();
+  for (int32_t t = begin; t < t1; t += 4) {
+    const int32_t k0 = t * BK;
+    const uint32_t missing = missing_of<BK>(pg, k0, it.kv, a.page_shift);
+    f32x16_t s[1];
+    uint32_t p[1][8];
+    wait_vm<V::kCopies>();  // the keys are here
+    w.scores(s, mine);
+    wait_vm<V::kCopies>();  // and read: their room is free
+    keys(t + 4);
+    w.softmax(a, s, p, k0, missing);
+    wait_vm<K::kCopies>();
+    w.values(p, mine + kTile);
+    wait_vm<K::kCopies>();
+    values(t + 4);
+  }
+  wait_vm<0>();
+  w.l = Wave<T, D, BK, CAP>::row_sum(w.l);
+
+  // The waves' sums, brought to one maximum and added in the waves' order.  Element
+  // d of row r of a wave is at word 32 d + (r + d) % 32 of its part.
+  const float c = CAP ? 1.f : a.scale2;
+  const int r = lane & 31, half = lane >> 5;
+  if (half == 0) ml[0][wv][r] = w.m * c, ml[1][wv][r] = w.l;
+  if (threadIdx.x == 0) again = 0;
+  __syncthreads();
+  float top = ml[0][0][r];
+#pragma unroll
+  for (int v = 1; v < 4; ++v) top = fmaxf(top, ml[0][v][r]);
+  // a NaN score's maximum is left out by fmaxf, its sum is not
+  const float f = w.m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(w.m * c - top);
+  float *const sums = reinterpret_cast<float *>(mine);
+#pragma unroll
+  for (int b = 0; b < D / 32; ++b)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const int d = 32 * b + 8 * (i / 4) + 4 * half + i % 4;
+      sums[32 * d + ((r + d) & 31)] = w.o[b][i] * f;
+    }
+  __syncthreads();
+  const bool split = it.splits > 1;
+  const int64_t item = (int64_t)kh * a.items + at;
+  const float *all = reinterpret_cast<const float *>(lds);
+  const int32_t rows = (int32_t)min((int64_t)32, (int64_t)it.n * a.group - (int64_t)it.tile * 32);
+  for (int32_t e = threadIdx.x; e < rows * (D / 4); e += 256) {
+    const int32_t rr = e / (D / 4), d0 = 4 * (e % (D / 4));
+    float mx = ml[0][0][rr], l = 0.f, v[4];
+#pragma unroll
+    for (int u = 1; u < 4; ++u) mx = fmaxf(mx, ml[0][u][rr]);
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const float mu = ml[0][u][rr];
+      l += ml[1][u][rr] * (mu == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mu - mx));
+    }
+    bool ok = l * 0.f == 0.f;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int d = d0 + j;
+      float x = 0.f;
+#pragma unroll
+      for (int u = 0; u < 4; ++u) x += all[u * (32 * D) + 32 * d + ((rr + d) & 31)];
+      v[j] = x;
+      ok = ok && x * 0.f == 0.f;
+    }
+    if (!ok) atomicOr(&again, 1u << rr);
+    int32_t tk, hd;
+    const int64_t rw = row_of(a, it, rr, kh, tk, hd);
+    if (split) {
+      float *dst = partial(a, item, rr, D);
+      *reinterpret_cast<float2 *>(dst + d0) = make_float2(v[0], v[1]);
+      *reinterpret_cast<float2 *>(dst + d0 + 2) = make_float2(v[2], v[3]);
+      if (d0 == 0) *reinterpret_cast<float2 *>(dst + D) = make_float2(mx, l);
+    } else {
+      const float inv = l != 0.f ? 1.f / l : 0.f;
+      *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(a.o.out) + rw * a.o.out_stride + (int64_t)hd * D + d0) =
+          make_uint2(pack2<T>(v[0] * inv, v[1] * inv), pack2<T>(v[2] * inv, v[3] * inv));
+    }
+  }
+  __syncthreads();
+  uint32_t todo = again;
+  for (; todo; todo &= todo - 1) {
+    const int src = __builtin_ctz(todo);
+    if (src % 4 != wv) continue;
+    const int32_t klo = max(__builtin_amdgcn_readlane(w.lo, src), t0 * BK);
+    const int32_t khi = min(__builtin_amdgcn_readlane(w.hi, src), t1 * BK);
+    int32_t tk, hd;
+    const int64_t rw = row_of(a, it, src, kh, tk, hd);
+    Row<T, D> x;
+    row_again<T, D, CAP>(a, static_cast<const uint16_t *>(a.o.q) + rw * a.o.q_stride + (int64_t)hd * D, ho,
+                         pg.table, pg.count, klo, khi, &x);
+    constexpr int E = D / 64;
+    if (split) {
+      float *dst = partial(a, item, src, D);
+#pragma unroll
+      for (int e = 0; e < E; ++e) dst[lane * E + e] = x.acc[e];
+      if (lane == 0) dst[D] = x.m * c, dst[D + 1] = x.l;
+    } else {
+      uint16_t *dst = static_cast<uint16_t *>(a.o.out) + rw * a.o.out_stride + (int64_t)hd * D;
+      const float inv = x.l != 0.f ? 1.f / x.l : 0.f;
+#pragma unroll
+      for (int e = 0; e < E; ++e) dst[lane * E + e] = to_y16(x.acc[e] * inv, T);
+    }
+  }
+}
+
+// Joins the splits of each row, in their order: one wave per row.
+template <int T, int D>
+__global__ void __launch_bounds__(256) attn_join_kernel(AttnArgs a) {
+  constexpr int E = D / 64;
+  const int lane = threadIdx.x & 63;
+  const int32_t kh = (int32_t)(blockIdx.x / a.items);
+  const int64_t at = blockIdx.x % a.items;
+  const Item it = find_item(a, at);
+  if (it.b < 0 || it.splits == 1 || it.split != 0 || at + it.splits > a.items) return;
+  for (int32_t r = (int32_t)(blockIdx.y * 4 + (threadIdx.x >> 6)); r < a.part_rows; r += 4 * gridDim.y) {
+    int32_t tok, head;
+    const int64_t row = row_of(a, it, r, kh, tok, head);
+    if (row < 0) return;
+    const int64_t item = (int64_t)kh * a.items + at;
+    float m = -INFINITY, l = 0.f, v[E] = {};
+    for (int32_t s = 0; s < it.splits; ++s) m = fmaxf(m, partial(a, item + s, r, D)[D]);
+    for (int32_t s = 0; s < it.splits; ++s) {
+      const float *src = partial(a, item + s, r, D);
+      const float f = src[D] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(src[D] - m);
+      l = __builtin_fmaf(src[D + 1], f, l);
+#pragma unroll
+      for (int e = 0; e < E; ++e) v[e] = __builtin_fmaf(src[lane * E + e], f, v[e]);
+    }
+    uint16_t *dst = static_cast<uint16_t *>(a.o.out) + row * a.o.out_stride + (int64_t)head * D + lane * E;
+    const float inv = l != 0.f ? 1.f / l : 0.f;
+#pragma unroll
+    for (int e = 0; e < E; ++e) dst[e] = to_y16(v[e] * inv, T);
+  }
+}
+
+template <int T, int D>
+hipError_t attn_launch_d(const AttnArgs &a, hipStream_t s) {
+  constexpr int BK = D == 256 ? 32 : 64;
+  const dim3 grid(a.grid_wgs);
+  const bool cap = a.cap2 != 0.f;
+  if (a.tile_rows == 128) {
+    if (cap)
+      attn_tile_kernel<T, D, BK, true><<<grid, 256, 0, s>>>(a);
+    else
+      attn_tile_kernel<T, D, BK, false><<<grid, 256, 0, s>>>(a);
+  } else {
+    if (cap)
+      attn_stream_kernel<T, D, true><<<grid, 256, 0, s>>>(a);
+    else
+      attn_stream_kernel<T, D, false><<<grid, 256, 0, s>>>(a);
+  }
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || a.target <= 0) return e;
+  const unsigned rows = (unsigned)((a.part_rows + 3) / 4);
+  attn_join_kernel<T, D><<<dim3(a.grid, rows), 256, 0, s>>>(a);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+template <int T>
+hipError_t attn_launch(const AttnArgs &a, hipStream_t s) {
+  switch (a.o.cache.dim) {
+    case 64: return attn_launch_d<T, 64>(a, s);
+    case 128: return attn_launch_d<T, 128>(a, s);
+    default: return attn_launch_d<T, 256>(a, s);
+  }
+}
+
+}  // namespace eb
+
+#endif  // EB_ATTENTION_TILE_H
