@@ -10,6 +10,7 @@
 namespace eb {
 
 constexpr int kMaxBatch = 4096;
+constexpr int kMaxSplits = 1024;  // of a row tile
 
 hipError_t launch_kv_extend(const eb_kv_extend_op &o, hipStream_t s);
 hipError_t launch_rope_append(const eb_rope_append_op &o, hipStream_t s);
@@ -29,7 +30,8 @@ struct AttnArgs {
   int32_t min_units;   // of a split
   int32_t target;      // items of a key/value head that splits may add; 0: no splits
   int32_t part_rows;   // rows of a tile that a split may have sums of
-  uint32_t items;      // of a key/value head, at most
+  uint32_t tiles;      // row tiles of all sequences, at most
+  uint32_t items;      // of a key/value head, at most: tiles + target
   uint32_t grid;       // items of all heads
   uint32_t grid_wgs;   // workgroups: grid rounded up to the XCDs
   uint32_t flip;       // sign bits of a pair of queries where the scale is negative

@@ -28,21 +28,26 @@ AttnArgs plan(const eb_attention_op &o) {
   }
   const int64_t max_new = o.max_new < o.rows ? o.max_new : o.rows;
   const int64_t rows = max_new * a.group;  // of a sequence and key/value head
-  a.tile_rows = rows <= 32 ? 32 : 128;
-  a.unit = a.tile_rows == 32 ? 128 : 64;
-  a.min_units = a.tile_rows == 32 ? 1 : 4;
+  const int64_t heads = o.cache.heads, cus = device_cu_count();
+  // row tiles of all sequences, at most
+  auto tiles_of = [&](int64_t tile_rows) {
+    const int64_t each = o.batch * ((rows + tile_rows - 1) / tile_rows);
+    const int64_t packed = (int64_t)o.rows * a.group / tile_rows + o.batch;
+    return o.batch > 1 && packed < each ? packed : each;
+  };
+  a.tile_rows = rows <= 32 || tiles_of(128) * heads < cus ? 32 : 128;
+  const int64_t tiles = tiles_of(a.tile_rows);
   a.part_rows = (int32_t)(rows < a.tile_rows ? rows : a.tile_rows);
-  const int64_t per_seq = (rows + a.tile_rows - 1) / a.tile_rows;
-  int64_t tiles = o.batch * per_seq;
-  const int64_t packed = (int64_t)o.rows * a.group / a.tile_rows + o.batch;
-  if (o.batch > 1 && packed < tiles) tiles = packed;
-  // Splits: where the tiles alone leave CUs idle, or one sequence of a batch
-  // may be far longer than the others.
-  const int64_t cus = device_cu_count();
-  const int64_t slots = 2 * cus;
-  const int64_t heads = o.cache.heads;
-  const bool longer = o.max_kv > a.unit * a.min_units;
-  if (longer && (o.batch > 1 || tiles * heads < slots)) a.target = (int32_t)((slots + heads - 1) / heads);
+  // Splits of the keys: where the tiles alone leave workgroup slots idle, or one
+  // sequence of a batch may be far longer than the others.
+  const int64_t slots = cus * (o.cache.dim == 256 ? 1 : 2);
+  a.unit = a.tile_rows == 32 ? 128 : 64;
+  a.min_units = a.tile_rows == 32 ? 1 : 16;
+  if (o.max_kv > a.unit * a.min_units && (o.batch > 1 || tiles * heads * 2 <= slots)) {
+    const int64_t target = (slots + heads - 1) / heads;
+    a.target = (int32_t)(target < kMaxSplits ? target : kMaxSplits);
+  }
+  a.tiles = (uint32_t)tiles;
   a.items = (uint32_t)(tiles + a.target);
   const int64_t grid = (int64_t)a.items * heads;
   a.grid = (uint32_t)grid;

@@ -82,28 +82,29 @@ __device__ inline int64_t wave_sum(int64_t v) {
 }
 
 // Item number `at` of a key/value head: the sequences' row tiles in order, each
-// `splits` times.  A sequence's tiles are split so that a split is at least
-// a.min_units units long and the splits of all sequences together about
-// a.target items (a longer sequence gets more); every wave of every workgroup
+// `splits` times (JOIN: once, and *base is its first item).  One sequence is
+// split as often as fits a.target items; of several, each into splits of at
+// least the U / a.target units that make the splits of all, U units together,
+// about a.target, so that a longer one gets more.  Every wave of every workgroup
 // finds the same numbers from the lengths.
-__device__ inline Item find_item(const AttnArgs &a, int64_t at) {
+template <bool JOIN>
+__device__ inline Item find_item(const AttnArgs &a, int64_t at, int64_t *base = nullptr) {
   const eb_attention_op &o = a.o;
   const int lane = threadIdx.x & 63;
   Item it;
-  Seq s;
+  Seq s{};
   int32_t splits = 1;
-  int64_t rest = at;
-  auto per_split = [&](int64_t units) {
-    const int64_t share = (units + a.target - 1) / a.target;
-    return share > a.min_units ? share : (int64_t)a.min_units;
-  };
-  auto splits_of = [&](const Seq &q, int64_t per) {
-    return a.target > 0 && q.units > 0 ? (int32_t)((q.units + per - 1) / per) : 1;
-  };
+  int64_t rest = at, first = 0;
   if (o.batch == 1) {
     s = seq_of(a, 0);
-    if (a.target > 0) splits = splits_of(s, per_split((int64_t)s.tiles * s.units));
-    if (at >= (int64_t)s.tiles * splits) return it;
+    if (a.target > 0) {
+      const int32_t most = min(a.target / max(s.tiles, 1), s.units / a.min_units);
+      if (most > 1) {
+        const int32_t per = (s.units + most - 1) / most;
+        splits = (s.units + per - 1) / per;
+      }
+    }
+    if (at >= (int64_t)s.tiles * (JOIN ? 1 : splits)) return it;
     it.b = 0;
   } else {
     int64_t per = 1;
@@ -112,30 +113,32 @@ __device__ inline Item find_item(const AttnArgs &a, int64_t at) {
       for (int32_t b0 = 0; b0 < o.batch; b0 += 64) {
         const int32_t b = b0 + lane;
         if (b < o.batch) {
-          const Seq q = seq_of(a, b);
-          units += (int64_t)q.tiles * q.units;
+          s = seq_of(a, b);
+          units += (int64_t)s.tiles * s.units;
         }
       }
-      per = per_split(wave_sum(units));
+      per = max((wave_sum(units) + a.target - 1) / a.target, (int64_t)a.min_units);
     }
     for (int32_t b0 = 0; b0 < o.batch; b0 += 64) {
       const int32_t b = b0 + lane;
-      int64_t items = 0;
+      int64_t items = 0, tiles = 0;
       if (b < o.batch) {
-        s = seq_of(a, b);
-        splits = splits_of(s, per);
-        items = (int64_t)s.tiles * splits;
+        if (a.target <= 0 || o.batch > 64) s = seq_of(a, b);  // (else it is here already)
+        splits = a.target > 0 && s.units > 0 ? (int32_t)((s.units + per - 1) / per) : 1;
+        tiles = s.tiles;
+        items = tiles * splits;
       }
-      int64_t sum = items;
+      int64_t sum = items, count = tiles;
 #pragma unroll
       for (int d = 1; d < 64; d <<= 1) {
-        const int64_t u = __shfl_up(sum, d);
-        if (lane >= d) sum += u;
+        const int64_t u = __shfl_up(sum, d), v = JOIN ? __shfl_up(count, d) : 0;
+        if (lane >= d) sum += u, count += v;
       }
-      const uint64_t past = __ballot(sum > rest);
+      const uint64_t past = __ballot((JOIN ? count : sum) > rest);
       if (past) {
         const int src = __builtin_ctzll(past);
-        rest -= __shfl(sum - items, src);
+        if (JOIN) first += __shfl(sum - items, src);
+        rest -= JOIN ? __shfl(count - tiles, src) : __shfl(sum - items, src);
         s.q0 = __shfl(s.q0, src);
         s.n = __shfl(s.n, src);
         s.p0 = __shfl(s.p0, src);
@@ -144,15 +147,18 @@ __device__ inline Item find_item(const AttnArgs &a, int64_t at) {
         it.b = b0 + src;
         break;
       }
-      rest -= __shfl(sum, 63);
+      if (JOIN) first += __shfl(sum, 63);
+      rest -= __shfl(JOIN ? count : sum, 63);
     }
     if (it.b < 0) return it;
   }
   auto uni = [](int32_t v) { return __builtin_amdgcn_readfirstlane(v); };
   it.b = uni(it.b);
   it.splits = uni(splits);
-  it.tile = uni((int32_t)(rest / it.splits));
-  it.split = uni((int32_t)(rest % it.splits));
+  const int32_t r = uni((int32_t)rest);
+  it.tile = JOIN ? r : r / it.splits;
+  it.split = JOIN ? 0 : r % it.splits;
+  if (JOIN) *base = first + (int64_t)r * it.splits;
   it.q0 = uni(s.q0);
   it.n = uni(s.n);
   it.p0 = uni(s.p0);
@@ -499,9 +505,13 @@ __device__ inline void row_again(const AttnArgs &a, const uint16_t *qrow, int64_
 // kernels
 // ---------------------------------------------------------------------------
 
-// Sums of a split, for rows [item][row of the tile]: D values, then m c and l.
-__device__ inline float *partial(const AttnArgs &a, int64_t item, int32_t row, int d) {
-  return a.ws + (item * a.part_rows + row) * (d + 2);
+// Sums of a split: D values of each row of the tile, and its maximum (times c) and
+// sum.
+__device__ inline float *part_o(const AttnArgs &a, int64_t item, int32_t row, int d) {
+  return a.ws + (item * a.part_rows + row) * d;
+}
+__device__ inline float2 *part_ml(const AttnArgs &a, int64_t item, int32_t row, int d) {
+  return reinterpret_cast<float2 *>(a.ws + (int64_t)a.grid * a.part_rows * d) + item * a.part_rows + row;
 }
 
 // This workgroup's item and key/value head.  Neighbouring workgroups go to the 8
@@ -573,7 +583,7 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) attn_tile_kernel(AttnAr
   int64_t at;
   locate(a, kh, at);
   if (kh >= a.o.cache.heads) return;
-  const Item it = find_item(a, at);
+  const Item it = find_item<false>(a, at);
   if (it.b < 0) return;
 
   Wave<T, D, BK, CAP> w;
@@ -641,14 +651,14 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) attn_tile_kernel(AttnAr
   const int half = lane >> 5;
   if (live) {
     if (split) {
-      float *dst = partial(a, item, 32 * wv + (lane & 31), D);
+      float *dst = part_o(a, item, 32 * wv + (lane & 31), D);
 #pragma unroll
       for (int b = 0; b < D / 32; ++b)
 #pragma unroll
-        for (int i = 0; i < 16; i += 2)
-          *reinterpret_cast<float2 *>(dst + 32 * b + 8 * (i / 4) + 4 * half + i % 4) =
-              make_float2(w.o[b][i], w.o[b][i + 1]);
-      if (half == 0) *reinterpret_cast<float2 *>(dst + D) = make_float2(w.m * c, w.l);
+        for (int i = 0; i < 16; i += 4)
+          *reinterpret_cast<float4 *>(dst + 32 * b + 8 * (i / 4) + 4 * half) =
+              make_float4(w.o[b][i], w.o[b][i + 1], w.o[b][i + 2], w.o[b][i + 3]);
+      if (half == 0) *part_ml(a, item, 32 * wv + (lane & 31), D) = make_float2(w.m * c, w.l);
     } else {
       uint16_t *dst = static_cast<uint16_t *>(a.o.out) + row * a.o.out_stride + (int64_t)head * D;
       const float inv = w.l != 0.f ? 1.f / w.l : 0.f;
@@ -676,10 +686,10 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) attn_tile_kernel(AttnAr
                          pg.table, pg.count, klo, khi, &r);
     constexpr int E = D / 64;
     if (split) {
-      float *dst = partial(a, item, 32 * wv + src, D);
+      float *dst = part_o(a, item, 32 * wv + src, D);
 #pragma unroll
       for (int e = 0; e < E; ++e) dst[lane * E + e] = r.acc[e];
-      if (lane == 0) dst[D] = r.m * c, dst[D + 1] = r.l;
+      if (lane == 0) *part_ml(a, item, 32 * wv + src, D) = make_float2(r.m * c, r.l);
     } else {
       uint16_t *dst = static_cast<uint16_t *>(a.o.out) + rw * a.o.out_stride + (int64_t)hd * D;
       const float inv = r.l != 0.f ? 1.f / r.l : 0.f;
@@ -707,7 +717,7 @@ __global__ void __launch_bounds__(256, 1) attn_stream_kernel(AttnArgs a) {
   int64_t at;
   locate(a, kh, at);
   if (kh >= a.o.cache.heads) return;
-  const Item it = find_item(a, at);
+  const Item it = find_item<false>(a, at);
   if (it.b < 0) return;
 
   Wave<T, D, BK, CAP> w;
@@ -811,10 +821,8 @@ __global__ void __launch_bounds__(256, 1) attn_stream_kernel(AttnArgs a) {
     int32_t tk, hd;
     const int64_t rw = row_of(a, it, rr, kh, tk, hd);
     if (split) {
-      float *dst = partial(a, item, rr, D);
-      *reinterpret_cast<float2 *>(dst + d0) = make_float2(v[0], v[1]);
-      *reinterpret_cast<float2 *>(dst + d0 + 2) = make_float2(v[2], v[3]);
-      if (d0 == 0) *reinterpret_cast<float2 *>(dst + D) = make_float2(mx, l);
+      *reinterpret_cast<float4 *>(part_o(a, item, rr, D) + d0) = make_float4(v[0], v[1], v[2], v[3]);
+      if (d0 == 0) *part_ml(a, item, rr, D) = make_float2(mx, l);
     } else {
       const float inv = l != 0.f ? 1.f / l : 0.f;
       *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(a.o.out) + rw * a.o.out_stride + (int64_t)hd * D + d0) =
@@ -835,10 +843,10 @@ __global__ void __launch_bounds__(256, 1) attn_stream_kernel(AttnArgs a) {
                          pg.table, pg.count, klo, khi, &x);
     constexpr int E = D / 64;
     if (split) {
-      float *dst = partial(a, item, src, D);
+      float *dst = part_o(a, item, src, D);
 #pragma unroll
       for (int e = 0; e < E; ++e) dst[lane * E + e] = x.acc[e];
-      if (lane == 0) dst[D] = x.m * c, dst[D + 1] = x.l;
+      if (lane == 0) *part_ml(a, item, src, D) = make_float2(x.m * c, x.l);
     } else {
       uint16_t *dst = static_cast<uint16_t *>(a.o.out) + rw * a.o.out_stride + (int64_t)hd * D;
       const float inv = x.l != 0.f ? 1.f / x.l : 0.f;
@@ -848,33 +856,85 @@ __global__ void __launch_bounds__(256, 1) attn_stream_kernel(AttnArgs a) {
   }
 }
 
-// Joins the splits of each row, in their order: one wave per row.
+// Joins the splits of a tile's rows, in an order that the number of splits decides.
+// D / 4 lanes read a row's sums at once, so a workgroup has 1024 / D places: with
+// few splits each takes a row of its own; with many, all take a part of one row's
+// splits (every 1024 / D-th) and their sums meet in LDS.
 template <int T, int D>
 __global__ void __launch_bounds__(256) attn_join_kernel(AttnArgs a) {
-  constexpr int E = D / 64;
-  const int lane = threadIdx.x & 63;
-  const int32_t kh = (int32_t)(blockIdx.x / a.items);
-  const int64_t at = blockIdx.x % a.items;
-  const Item it = find_item(a, at);
-  if (it.b < 0 || it.splits == 1 || it.split != 0 || at + it.splits > a.items) return;
-  for (int32_t r = (int32_t)(blockIdx.y * 4 + (threadIdx.x >> 6)); r < a.part_rows; r += 4 * gridDim.y) {
+  constexpr int kLanes = D / 4, kPlaces = 256 / kLanes;
+  __shared__ float weight[kMaxSplits];
+  __shared__ float red[8];
+  __shared__ float4 part[256];
+  const int32_t kh = (int32_t)(blockIdx.x / a.tiles);
+  int64_t base;
+  const Item it = find_item<true>(a, blockIdx.x % a.tiles, &base);
+  if (it.b < 0 || it.splits == 1 || it.splits > kMaxSplits || base + it.splits > a.items) return;
+  base += (int64_t)kh * a.items;
+  const int place = threadIdx.x / kLanes, d0 = 4 * (threadIdx.x % kLanes);
+  const int32_t rows =
+      (int32_t)min((int64_t)a.tile_rows, (int64_t)it.n * a.group - (int64_t)it.tile * a.tile_rows);
+  auto store = [&](int32_t r, float4 v, float l) {
     int32_t tok, head;
     const int64_t row = row_of(a, it, r, kh, tok, head);
-    if (row < 0) return;
-    const int64_t item = (int64_t)kh * a.items + at;
-    float m = -INFINITY, l = 0.f, v[E] = {};
-    for (int32_t s = 0; s < it.splits; ++s) m = fmaxf(m, partial(a, item + s, r, D)[D]);
-    for (int32_t s = 0; s < it.splits; ++s) {
-      const float *src = partial(a, item + s, r, D);
-      const float f = src[D] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(src[D] - m);
-      l = __builtin_fmaf(src[D + 1], f, l);
-#pragma unroll
-      for (int e = 0; e < E; ++e) v[e] = __builtin_fmaf(src[lane * E + e], f, v[e]);
-    }
-    uint16_t *dst = static_cast<uint16_t *>(a.o.out) + row * a.o.out_stride + (int64_t)head * D + lane * E;
     const float inv = l != 0.f ? 1.f / l : 0.f;
+    *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(a.o.out) + row * a.o.out_stride + (int64_t)head * D + d0) =
+        make_uint2(pack2<T>(v.x * inv, v.y * inv), pack2<T>(v.z * inv, v.w * inv));
+  };
+  auto add = [](float4 &v, const float4 &x, float f) {
+    v.x = __builtin_fmaf(x.x, f, v.x);
+    v.y = __builtin_fmaf(x.y, f, v.y);
+    v.z = __builtin_fmaf(x.z, f, v.z);
+    v.w = __builtin_fmaf(x.w, f, v.w);
+  };
+  if (it.splits <= kPlaces) {
+    for (int32_t r = blockIdx.y * kPlaces + place; r < rows; r += gridDim.y * kPlaces) {
+      float m = -INFINITY, l = 0.f;
+      for (int32_t s = 0; s < it.splits; ++s) m = fmaxf(m, part_ml(a, base + s, r, D)->x);
+      float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+      for (int32_t s = 0; s < it.splits; ++s) {
+        const float2 ml = *part_ml(a, base + s, r, D);
+        const float f = ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml.x - m);
+        l = __builtin_fmaf(ml.y, f, l);
+        add(v, *reinterpret_cast<const float4 *>(part_o(a, base + s, r, D) + d0), f);
+      }
+      store(r, v, l);
+    }
+    return;
+  }
+  const int wv = threadIdx.x >> 6;
+  for (int32_t r = blockIdx.y; r < rows; r += gridDim.y) {
+    float m = -INFINITY, l = 0.f;
+    for (int32_t s = threadIdx.x; s < it.splits; s += 256) m = fmaxf(m, part_ml(a, base + s, r, D)->x);
 #pragma unroll
-    for (int e = 0; e < E; ++e) dst[e] = to_y16(v[e] * inv, T);
+    for (int d = 32; d >= 1; d >>= 1) m = fmaxf(m, __shfl_xor(m, d));
+    if ((threadIdx.x & 63) == 0) red[wv] = m;
+    __syncthreads();
+    m = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+    for (int32_t s = threadIdx.x; s < it.splits; s += 256) {
+      const float2 ml = *part_ml(a, base + s, r, D);
+      const float f = ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml.x - m);
+      weight[s] = f;
+      l = __builtin_fmaf(ml.y, f, l);
+    }
+#pragma unroll
+    for (int d = 32; d >= 1; d >>= 1) l += __shfl_xor(l, d);
+    if ((threadIdx.x & 63) == 0) red[4 + wv] = l;
+    __syncthreads();
+    l = (red[4] + red[5]) + (red[6] + red[7]);
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 8
+    for (int32_t s = place; s < it.splits; s += kPlaces)
+      add(v, *reinterpret_cast<const float4 *>(part_o(a, base + s, r, D) + d0), weight[s]);
+    part[threadIdx.x] = v;
+    __syncthreads();
+    if (place == 0) {
+#pragma unroll
+      for (int q = 1; q < kPlaces; ++q) add(v, part[q * kLanes + threadIdx.x], 1.f);
+      store(r, v, l);
+    }
+    __syncthreads();
   }
 }
 
@@ -896,8 +956,11 @@ hipError_t attn_launch_d(const AttnArgs &a, hipStream_t s) {
   }
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.target <= 0) return e;
-  const unsigned rows = (unsigned)((a.part_rows + 3) / 4);
-  attn_join_kernel<T, D><<<dim3(a.grid, rows), 256, 0, s>>>(a);
+  // a workgroup per row, up to 2048 of them
+  const uint32_t tiles = a.tiles * (uint32_t)a.o.cache.heads;
+  const uint32_t most = tiles >= 2048 ? 1 : 2048 / tiles;
+  attn_join_kernel<T, D>
+      <<<dim3(tiles, (uint32_t)a.part_rows < most ? (uint32_t)a.part_rows : most), 256, 0, s>>>(a);
   return hipGetLastError();
 }
 

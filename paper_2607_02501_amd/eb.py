@@ -517,11 +517,11 @@ lib.eb_attention_workspace_bytes.argtypes = [ctypes.POINTER(eb_attention_op)]
 lib.eb_attention.restype = _i32
 lib.eb_attention.argtypes = [ctypes.POINTER(eb_attention_op), _vp, ctypes.c_size_t, _vp]
 _kv_extend, _rope_append, _attention = _raw.eb_kv_extend, _raw.eb_rope_append, _raw.eb_attention
-_attention_ws = _raw.eb_attention_workspace_bytes
 for _f in (_kv_extend, _rope_append):
     _f.restype, _f.argtypes = _i32, [ctypes.c_char_p, _vp]
 _attention.restype, _attention.argtypes = _i32, [ctypes.c_char_p, _vp, ctypes.c_size_t, _vp]
-_attention_ws.restype, _attention_ws.argtypes = ctypes.c_size_t, [ctypes.c_char_p]
+_raw.eb_attention_workspace_bytes.restype = ctypes.c_size_t
+_raw.eb_attention_workspace_bytes.argtypes = [ctypes.c_char_p]
 _ATTN_WS_BYTES = {}  # at most 4096 entries
 
 
@@ -531,44 +531,51 @@ def _need(ok: bool, what: str) -> None:
         raise ValueError(what)
 
 
-def _ints(name: str, t: torch.Tensor, device, *shape) -> int:
-    _need(t.dtype == torch.int32 and t.device == device and t.is_contiguous()
-          and (not shape or tuple(t.shape) == shape),
-          f"{name}: a contiguous int32 tensor on {device}" + (f" of shape {shape}" if shape else ""))
+# At one token these kernels take 3 to 10 us, so the host's part of a call counts:
+# the checks below are a few attribute reads each (0.3 us a tensor).
+
+def _ints(name: str, t: torch.Tensor, dev: int, n: int) -> int:
+    """The address of n contiguous int32 values on GPU `dev`."""
+    if t.dtype is not torch.int32 or t.get_device() != dev or t.numel() != n or not t.is_contiguous():
+        raise ValueError(f"{name}: {n} contiguous int32 values on cuda:{dev}")
     return t.data_ptr()
 
 
-def _floats(name: str, t: torch.Tensor | None, device, n: int) -> int:
+def _floats(name: str, t: torch.Tensor | None, dev: int, n: int) -> int:
     if t is None:
         return 0
-    _need(t.dtype == torch.float32 and t.device == device and t.is_contiguous() and t.numel() == n,
-          f"{name}: {n} contiguous float32 values on {device}")
+    if t.dtype is not torch.float32 or t.get_device() != dev or t.numel() != n or not t.is_contiguous():
+        raise ValueError(f"{name}: {n} contiguous float32 values on cuda:{dev}")
     return t.data_ptr()
 
 
-def _rows(name: str, t: torch.Tensor, device, dtype, width: int) -> int:
-    """Stride between the rows of t, whose first row axis may be strided."""
-    inner = t.shape[1:].numel()
-    _need(t.device == device and t.dtype == dtype and t.dim() >= 2 and inner == width
-          and (t.shape[0] == 0 or t[0].is_contiguous()),
-          f"{name}: rows of {width} {dtype} values on {device}")
-    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), width)
+def _heads(name: str, t: torch.Tensor, dev: int, dtype, rows: int, heads: int, dim: int) -> int:
+    """Stride between the rows of t [rows, heads, dim], whose rows are contiguous."""
+    if t.dtype is not dtype or t.get_device() != dev or t.shape != (rows, heads, dim):
+        raise ValueError(f"{name}: {dtype} values of shape {(rows, heads, dim)} on cuda:{dev}")
+    stride, head, elem = t.stride()
+    if elem != 1 or (head != dim and heads != 1):
+        raise ValueError(f"{name}: rows of contiguous heads")
+    return stride if rows > 1 else heads * dim
 
 
-class _on:
-    """Makes `device` current for a launch, where it is not."""
+_get_device = torch._C._cuda_getDevice
 
-    def __init__(self, device):
-        self.to, self.was = device.index, torch.cuda.current_device()
 
-    def __enter__(self):
-        if self.to != self.was:
-            torch.cuda.set_device(self.to)
-        return _raw_stream(self.to)
+def _launch(fn, op: bytes, dev: int, *more) -> int:
+    """fn(op, *more, stream) with GPU `dev` current, on its current stream."""
+    was = _get_device()
+    if was == dev:
+        return fn(op, *more, _raw_stream(dev))
+    torch.cuda.set_device(dev)
+    try:
+        return fn(op, *more, _raw_stream(dev))
+    finally:
+        torch.cuda.set_device(was)
 
-    def __exit__(self, *exc):
-        if self.to != self.was:
-            torch.cuda.set_device(self.was)
+
+def _attention_ws(op: bytes, stream: int) -> int:
+    return _raw.eb_attention_workspace_bytes(op)
 
 
 class KVCache:
@@ -582,18 +589,8 @@ class KVCache:
               "k and v: contiguous [pages, heads, page, dim] of float16 or bfloat16 on one GPU")
         self.k, self.v = k, v
         self.pages, self.heads, self.page, self.dim = k.shape
-
-    @property
-    def device(self):
-        return self.k.device
-
-    @property
-    def dtype(self):
-        return self.k.dtype
-
-    def fields(self) -> tuple:
-        return (self.k.data_ptr(), self.v.data_ptr(), DTYPES[self.k.dtype], self.heads, self.dim,
-                self.page, self.pages, 0)
+        self.device, self.dtype, self.index = k.device, k.dtype, k.get_device()
+        self.shape = (DTYPES[k.dtype], self.heads, self.dim, self.page, self.pages, 0)
 
 
 def empty_kv_cache(pages: int, page: int, heads: int, dim: int, dtype=torch.bfloat16,
@@ -604,14 +601,15 @@ def empty_kv_cache(pages: int, page: int, heads: int, dim: int, dtype=torch.bflo
 
 
 class KVBatch:
-    """What eb_kv_extend writes beside the block table (int32, on the GPU)."""
+    """What eb_kv_extend writes beside the block table (int32, on the GPU): one buffer
+    of q_start, kv_len, slots, positions, the pages left and the tokens without a page."""
 
     def __init__(self, batch: int, rows: int, device):
-        # one buffer: q_start, kv_len, slots, positions, pages left, tokens without a page
+        self.batch, self.rows = batch, rows
         sizes = (batch + 1, batch, rows, rows, 1, 1)
-        buf = torch.empty(sum(sizes), dtype=torch.int32, device=device)
+        self.buf = torch.empty(2 * (batch + rows) + 3, dtype=torch.int32, device=device)
         self.q_start, self.kv_len, self.slots, self.positions, self.n_free, self.short = \
-            buf.split(sizes)
+            torch.split_with_sizes(self.buf, sizes)
 
 
 def kv_extend(table: torch.Tensor, cached: torch.Tensor, added: torch.Tensor,
@@ -621,19 +619,21 @@ def kv_extend(table: torch.Tensor, cached: torch.Tensor, added: torch.Tensor,
     [batch, stride] gets the new pages' entries in place; the lengths, slots and
     positions of a step of `rows` rows are returned.  n_free stays as it was:
     the pages left are the result's n_free."""
-    dev = table.device
-    _need(table.is_cuda and table.dim() == 2, "table: [batch, stride] on a GPU")
+    dev = table.get_device()
+    _need(dev >= 0 and table.dim() == 2, "table: [batch, stride] on a GPU")
     batch, stride = table.shape
-    out = out or KVBatch(batch, rows, dev)
+    if out is None:
+        out = KVBatch(batch, rows, table.device)
+    _need(out.batch == batch and out.rows == rows, "out: a KVBatch of this batch and these rows")
+    free = free_pages.numel()
+    at = _ints("out", out.buf, dev, 2 * (batch + rows) + 3)
+    lens, slots = at + 4 * (batch + 1), at + 4 * (2 * batch + 1)
     op = _PACK_EXTEND.pack(
         _ints("cached", cached, dev, batch), _ints("added", added, dev, batch),
-        _ints("table", table, dev), _ints("free_pages", free_pages, dev),
-        _ints("n_free", n_free, dev, 1), _ints("n_free", out.n_free, dev, 1),
-        _ints("q_start", out.q_start, dev, batch + 1), _ints("kv_len", out.kv_len, dev, batch),
-        _ints("slots", out.slots, dev, rows), _ints("positions", out.positions, dev, rows),
-        _ints("short", out.short, dev, 1), batch, rows, page, pages, stride, free_pages.numel())
-    with _on(dev) as stream:
-        _check(_kv_extend(op, stream), "eb_kv_extend")
+        _ints("table", table, dev, batch * stride), _ints("free_pages", free_pages, dev, free),
+        _ints("n_free", n_free, dev, 1), slots + 8 * rows, at, lens, slots if rows else 0,
+        slots + 4 * rows if rows else 0, slots + 8 * rows + 4, batch, rows, page, pages, stride, free)
+    _check(_launch(_kv_extend, op, dev), "eb_kv_extend")
     return out
 
 
@@ -646,30 +646,30 @@ def rope_append(qkv: torch.Tensor, cache: KVCache, slots: torch.Tensor, position
     and values go to `cache` at `slots`.  positions: [rows], or [axes, rows] with
     `sections` (rotated pairs along each axis); freqs: radians per position of
     each rotated pair, 2 * len(freqs) elements of a head being rotated."""
-    dev, dim = cache.device, cache.dim
+    dev, dim = cache.index, cache.dim
+    width = (q_heads + 2 * cache.heads) * dim
+    _need(qkv.dim() == 2 and qkv.shape[1] == width and qkv.get_device() == dev and qkv.dtype in DTYPES
+          and qkv.stride(1) == 1,
+          f"qkv: rows of {width} float32, float16 or bfloat16 values on cuda:{dev}")
     rows = qkv.shape[0]
-    stride = _rows("qkv", qkv, dev, qkv.dtype, (q_heads + 2 * cache.heads) * dim)
-    _need(qkv.dtype in DTYPES, "qkv: float32, float16 or bfloat16")
     if out is None:
-        out = torch.empty((rows, q_heads, dim), dtype=cache.dtype, device=dev)
-    _need(out.shape[0] == rows, "out: a row for each row of qkv")
-    q_stride = _rows("out", out, dev, cache.dtype, q_heads * dim)
+        out = torch.empty((rows, q_heads, dim), dtype=cache.dtype, device=cache.device)
+    q_stride = _heads("out", out, dev, cache.dtype, rows, q_heads, dim)
     half = freqs.numel() if freqs is not None else 0
     axes, pos, pos_stride = 1, 0, 0
     if half:
-        _need(positions is not None and positions.dim() <= 2 and positions.shape[-1] == rows,
-              "positions: [rows] or [axes, rows]")
+        _need(positions is not None and positions.dim() <= 2, "positions: [rows] or [axes, rows]")
         axes = positions.shape[0] if positions.dim() == 2 else 1
-        pos, pos_stride = _ints("positions", positions, dev), rows
+        pos, pos_stride = _ints("positions", positions, dev, axes * rows), rows
     sections = tuple(sections) if sections is not None else (half,)
     _need(len(sections) == axes and axes <= 3, "sections: rotated pairs for each of up to 3 axes")
     op = _PACK_ROPE.pack(
-        *cache.fields(), qkv.data_ptr(), out.data_ptr(), _ints("slots", slots, dev, rows), pos,
-        _floats("freqs", freqs, dev, half), _floats("q_norm", q_norm, dev, dim),
-        _floats("k_norm", k_norm, dev, dim), stride, q_stride, pos_stride, DTYPES[qkv.dtype], q_heads,
-        rows, 2 * half, STYLES[style], axes, *(sections + (0, 0))[:3], float(eps))
-    with _on(dev) as stream:
-        _check(_rope_append(op, stream), "eb_rope_append")
+        cache.k.data_ptr(), cache.v.data_ptr(), *cache.shape, qkv.data_ptr(), out.data_ptr(),
+        _ints("slots", slots, dev, rows), pos, _floats("freqs", freqs, dev, half),
+        _floats("q_norm", q_norm, dev, dim), _floats("k_norm", k_norm, dev, dim),
+        qkv.stride(0) if rows > 1 else width, q_stride, pos_stride, DTYPES[qkv.dtype], q_heads, rows,
+        2 * half, STYLES[style], axes, *(sections + (0, 0))[:3], eps)
+    _check(_launch(_rope_append, op, dev), "eb_rope_append")
     return out
 
 
@@ -683,43 +683,45 @@ def attention(q: torch.Tensor, cache: KVCache, table: torch.Tensor, q_start: tor
     given.  workspace: a uint8 tensor of attention_workspace_bytes bytes; without
     one the call takes one from scratch(), or, under graph capture, a fresh one
     that belongs to the graph."""
-    dev, dim = cache.device, cache.dim
-    _need(q.dim() == 3 and q.shape[2] == dim, "q: [rows, q_heads, dim]")
+    dev, dim = cache.index, cache.dim
+    _need(q.dim() == 3 and table.dim() == 2, "q: [rows, q_heads, dim]; table: [batch, stride]")
     rows, q_heads, _ = q.shape
-    _need(table.dim() == 2, "table: [batch, stride]")
-    batch, table_stride = table.shape
-    q_stride = _rows("q", q, dev, cache.dtype, q_heads * dim)
+    batch, stride = table.shape
+    q_stride = _heads("q", q, dev, cache.dtype, rows, q_heads, dim)
     if out is None:
-        out = torch.empty((rows, q_heads, dim), dtype=cache.dtype, device=dev)
-    _need(out.shape[0] == rows, "out: a row for each row of q")
-    out_stride = _rows("out", out, dev, cache.dtype, q_heads * dim)
-    if scale is None:
-        scale = dim ** -0.5
+        out = torch.empty((rows, q_heads, dim), dtype=cache.dtype, device=cache.device)
+        out_stride = q_heads * dim
+    else:
+        out_stride = _heads("out", out, dev, cache.dtype, rows, q_heads, dim)
     op = _PACK_ATTN.pack(
-        *cache.fields(), q.data_ptr(), out.data_ptr(), _ints("table", table, dev),
-        _ints("q_start", q_start, dev, batch + 1), _ints("kv_len", kv_len, dev, batch),
-        _ints("prefix", prefix, dev, batch) if prefix is not None else 0, q_stride, out_stride, rows,
-        batch, q_heads, table_stride, max_new, max_kv, MASKS[mask], window, scale, softcap)
-    with _on(dev) as stream:
-        if workspace is None:
-            # what the size depends on (the current device's CU count too)
-            key = (rows, batch, q_heads, cache.heads, dim, max_new, max_kv, mask, dev.index)
-            nbytes = _ATTN_WS_BYTES.get(key)
-            if nbytes is None:
-                nbytes = _attention_ws(op)  # 0 too for a call that will be refused
-            if not nbytes:
-                workspace = None
-            elif torch.cuda.is_current_stream_capturing():
-                workspace = torch.empty(nbytes, dtype=torch.uint8, device=dev)
-            else:
-                workspace = scratch(dev, nbytes)
+        cache.k.data_ptr(), cache.v.data_ptr(), *cache.shape, q.data_ptr(), out.data_ptr(),
+        _ints("table", table, dev, batch * stride), _ints("q_start", q_start, dev, batch + 1),
+        _ints("kv_len", kv_len, dev, batch), _ints("prefix", prefix, dev, batch) if prefix is not None else 0,
+        q_stride, out_stride, rows, batch, q_heads, stride, max_new, max_kv, MASKS[mask], window,
+        dim ** -0.5 if scale is None else scale, softcap)
+    if workspace is not None:
+        _need(workspace.dtype is torch.uint8 and workspace.get_device() == dev and workspace.is_contiguous(),
+              f"workspace: contiguous uint8 on cuda:{dev}")
+        _check(_launch(_attention, op, dev, workspace.data_ptr(), workspace.numel()), "eb_attention")
+        return out
+    # its size, by what it depends on, is kept after a call that succeeded
+    key = (rows, batch, q_heads, cache.heads, dim, max_new, max_kv, dev)
+    nbytes = _ATTN_WS_BYTES.get(key)
+    known = nbytes is not None
+    if not known:
+        nbytes = _launch(_attention_ws, op, dev)  # 0 too for a call that will be refused
+    if not nbytes:
+        st = _launch(_attention, op, dev, None, 0)
+    else:
+        if torch.cuda.is_current_stream_capturing():
+            ws = torch.empty(nbytes, dtype=torch.uint8, device=cache.device)
         else:
-            key = nbytes = None
-            _need(workspace.dtype == torch.uint8 and workspace.device == dev
-                  and workspace.is_contiguous(), f"workspace: contiguous uint8 on {dev}")
-        _check(_attention(op, workspace.data_ptr() if workspace is not None else None,
-                          workspace.numel() if workspace is not None else 0, stream), "eb_attention")
-    if key is not None and key not in _ATTN_WS_BYTES:
+            ws = _SCRATCH.get((dev, _raw_stream(dev)))
+            if ws is None or ws.numel() < nbytes:
+                ws = scratch(cache.device, nbytes)
+        st = _launch(_attention, op, dev, ws.data_ptr(), ws.numel())
+    _check(st, "eb_attention")
+    if not known:
         if len(_ATTN_WS_BYTES) >= 4096:
             _ATTN_WS_BYTES.clear()
         _ATTN_WS_BYTES[key] = nbytes
@@ -727,11 +729,11 @@ def attention(q: torch.Tensor, cache: KVCache, table: torch.Tensor, q_start: tor
 
 
 def attention_workspace_bytes(q_shape, cache: KVCache, batch: int, table_stride: int, max_new: int,
-                              max_kv: int, mask: str = "causal") -> int:
+                              max_kv: int) -> int:
     """Bytes of workspace that attention() needs for queries of q_shape."""
     rows, q_heads, dim = q_shape
     w, stand_in = q_heads * dim, cache.k.data_ptr()  # pointers are only checked for alignment
-    op = _PACK_ATTN.pack(*cache.fields(), stand_in, stand_in, stand_in, stand_in, stand_in, 0, w, w, rows,
-                         batch, q_heads, table_stride, max_new, max_kv, MASKS[mask], 0, 1.0, 0.0)
-    with _on(cache.device):
-        return int(_attention_ws(op))
+    op = _PACK_ATTN.pack(stand_in, stand_in, *cache.shape, stand_in, stand_in, stand_in, stand_in,
+                         stand_in, 0, w, w, rows, batch, q_heads, table_stride, max_new, max_kv,
+                         EB_MASK_CAUSAL, 0, 1.0, 0.0)
+    return int(_launch(_attention_ws, op, cache.index))
