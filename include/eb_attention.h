@@ -173,7 +173,7 @@ typedef struct {
   const int32_t *prefix;  /* [batch], or null: no prefix */
   int64_t q_stride;       /* elements, >= q_heads * dim, a multiple of 8 */
   int64_t out_stride;     /* elements, >= q_heads * dim, a multiple of 8 */
-  int32_t rows;           /* 0 .. 2^24 */
+  int32_t rows;           /* 0 .. 2^24, rows * q_heads / heads <= 2^30 */
   int32_t batch;          /* 1 .. 4096 */
   int32_t q_heads;        /* a multiple of the cache's heads, at most 4096 */
   int32_t table_stride;   /* >= 1, table_stride * page <= 2^30 */

@@ -34,6 +34,7 @@ struct AttnArgs {
   uint32_t items;      // of a key/value head, at most: tiles + target
   uint32_t grid;       // items of all heads
   uint32_t grid_wgs;   // workgroups: grid rounded up to the XCDs
+  bool spread;         // one row tile a sequence: workgroups in order of item
   uint32_t flip;       // sign bits of a pair of queries where the scale is negative
   float scale2;        // 2^(scale2 s) without a cap; 2^(scale2 s) = e^(2 scale s / cap) with one
   float cap2;          // cap * log2 e, 0 without a cap

@@ -40,7 +40,8 @@ AttnArgs plan(const eb_attention_op &o) {
   a.part_rows = (int32_t)(rows < a.tile_rows ? rows : a.tile_rows);
   // Splits of the keys: where the tiles alone leave workgroup slots idle, or one
   // sequence of a batch may be far longer than the others.
-  const int64_t slots = cus * (o.cache.dim == 256 ? 1 : 2);
+  // (workgroups on a CU: see kStreamWgs and the tile kernel's launch bounds)
+  const int64_t slots = cus * (o.cache.dim == 256 ? 1 : o.cache.dim == 64 && a.tile_rows == 32 ? 3 : 2);
   a.unit = a.tile_rows == 32 ? 128 : 64;
   a.min_units = a.tile_rows == 32 ? 1 : 16;
   if (o.max_kv > a.unit * a.min_units && (o.batch > 1 || tiles * heads * 2 <= slots)) {
@@ -48,6 +49,7 @@ AttnArgs plan(const eb_attention_op &o) {
     a.target = (int32_t)(target < kMaxSplits ? target : kMaxSplits);
   }
   a.tiles = (uint32_t)tiles;
+  a.spread = rows <= a.tile_rows;
   a.items = (uint32_t)(tiles + a.target);
   const int64_t grid = (int64_t)a.items * heads;
   a.grid = (uint32_t)grid;

@@ -128,7 +128,8 @@ eb_status check_attention(const eb_attention_op &o) {
   if (st != EB_OK) return st;
   const int64_t width = (int64_t)o.q_heads * o.cache.dim;
   if (o.rows < 0 || o.rows > kMaxRows || o.batch < 1 || o.batch > kMaxBatch || o.q_heads < 1 ||
-      o.q_heads > 4096 || o.q_heads % o.cache.heads != 0 || o.q_stride < width || o.out_stride < width ||
+      o.q_heads > 4096 || o.q_heads % o.cache.heads != 0 ||
+      (int64_t)o.rows * (o.q_heads / o.cache.heads) > kMaxKeys || o.q_stride < width || o.out_stride < width ||
       o.q_stride > kMaxInt || o.out_stride > kMaxInt || o.table_stride < 1 ||
       (int64_t)o.table_stride * o.cache.page > kMaxKeys || o.max_new < 1 || o.max_kv < 1 || o.window < 0 ||
       (o.mask != EB_MASK_CAUSAL && o.mask != EB_MASK_FULL))

@@ -47,12 +47,13 @@ typedef short s16x4_t __attribute__((ext_vector_type(4)));
 // ---------------------------------------------------------------------------
 
 struct Item {
-  int32_t b = -1;        // sequence, -1: none
-  int32_t tile = 0;      // row tile of the sequence
+  int32_t b = -1;         // sequence, -1: none
   int32_t split = 0, splits = 1;
   int32_t q0 = 0, n = 0;  // first row of q, new tokens to compute
-  int32_t p0 = 0;        // place of the first new token
+  int32_t p0 = 0;         // place of the first new token
   int32_t kv = 0;
+  int32_t rows = 0;       // of the tile
+  int32_t tok0 = 0, head0 = 0;  // of the tile's first row
 };
 
 struct Seq {
@@ -67,18 +68,13 @@ __device__ inline Seq seq_of(const AttnArgs &a, int32_t b) {
   s.q0 = r0;
   s.p0 = s.kv - (r1 - r0);
   s.n = min(r1 - r0, o.max_new);
-  s.tiles = (int32_t)(((int64_t)s.n * a.group + a.tile_rows - 1) / a.tile_rows);
+  s.tiles = (s.n * a.group + a.tile_rows - 1) / a.tile_rows;
   // units of keys that a tile may see
-  int64_t see = s.kv;
-  if (o.window > 0 && o.mask != EB_MASK_FULL && !o.prefix) see = min(see, (int64_t)o.window + a.tile_rows);
-  s.units = (int32_t)((see + a.unit - 1) / a.unit);
+  int32_t see = s.kv;
+  if (o.window > 0 && o.window < see && o.mask != EB_MASK_FULL && !o.prefix)
+    see = min(see, o.window + a.tile_rows);
+  s.units = (see + a.unit - 1) / a.unit;
   return s;
-}
-
-__device__ inline int64_t wave_sum(int64_t v) {
-#pragma unroll
-  for (int d = 32; d >= 1; d >>= 1) v += __shfl_xor(v, d);
-  return v;
 }
 
 // Item number `at` of a key/value head: the sequences' row tiles in order, each
@@ -88,13 +84,13 @@ __device__ inline int64_t wave_sum(int64_t v) {
 // about a.target, so that a longer one gets more.  Every wave of every workgroup
 // finds the same numbers from the lengths.
 template <bool JOIN>
-__device__ inline Item find_item(const AttnArgs &a, int64_t at, int64_t *base = nullptr) {
+__device__ inline Item find_item(const AttnArgs &a, uint32_t at, uint32_t *base = nullptr) {
   const eb_attention_op &o = a.o;
   const int lane = threadIdx.x & 63;
+  auto uni = [](int32_t v) { return __builtin_amdgcn_readfirstlane(v); };
   Item it;
   Seq s{};
-  int32_t splits = 1;
-  int64_t rest = at, first = 0;
+  uint32_t rest = at, first = 0, splits = 1;
   if (o.batch == 1) {
     s = seq_of(a, 0);
     if (a.target > 0) {
@@ -104,65 +100,70 @@ __device__ inline Item find_item(const AttnArgs &a, int64_t at, int64_t *base = 
         splits = (s.units + per - 1) / per;
       }
     }
-    if (at >= (int64_t)s.tiles * (JOIN ? 1 : splits)) return it;
+    if (at >= s.tiles * (JOIN ? 1 : splits)) return it;
     it.b = 0;
+    it.splits = uni(splits);
   } else {
-    int64_t per = 1;
+    uint32_t per = 1;
     if (a.target > 0) {
-      int64_t units = 0;
+      float units = 0.f;  // exact below 2^24
       for (int32_t b0 = 0; b0 < o.batch; b0 += 64) {
         const int32_t b = b0 + lane;
         if (b < o.batch) {
           s = seq_of(a, b);
-          units += (int64_t)s.tiles * s.units;
+          units += (float)s.tiles * (float)s.units;
         }
       }
-      per = max((wave_sum(units) + a.target - 1) / a.target, (int64_t)a.min_units);
+#pragma unroll
+      for (int d = 32; d >= 1; d >>= 1) units += __shfl_xor(units, d);
+      per = units < 16777216.f ? ((uint32_t)units + a.target - 1) / a.target : (uint32_t)(units / a.target) + 2;
+      per = max(per, (uint32_t)a.min_units);
     }
     for (int32_t b0 = 0; b0 < o.batch; b0 += 64) {
       const int32_t b = b0 + lane;
-      int64_t items = 0, tiles = 0;
+      uint32_t items = 0, tiles = 0;
       if (b < o.batch) {
         if (a.target <= 0 || o.batch > 64) s = seq_of(a, b);  // (else it is here already)
-        splits = a.target > 0 && s.units > 0 ? (int32_t)((s.units + per - 1) / per) : 1;
+        splits = a.target > 0 && s.units > 0 ? (s.units + per - 1) / per : 1;
         tiles = s.tiles;
         items = tiles * splits;
       }
-      int64_t sum = items, count = tiles;
+      uint32_t sum = items, count = tiles;
 #pragma unroll
       for (int d = 1; d < 64; d <<= 1) {
-        const int64_t u = __shfl_up(sum, d), v = JOIN ? __shfl_up(count, d) : 0;
+        const uint32_t u = __shfl_up(sum, d), v = JOIN ? __shfl_up(count, d) : 0;
         if (lane >= d) sum += u, count += v;
       }
       const uint64_t past = __ballot((JOIN ? count : sum) > rest);
       if (past) {
         const int src = __builtin_ctzll(past);
-        if (JOIN) first += __shfl(sum - items, src);
-        rest -= JOIN ? __shfl(count - tiles, src) : __shfl(sum - items, src);
-        s.q0 = __shfl(s.q0, src);
-        s.n = __shfl(s.n, src);
-        s.p0 = __shfl(s.p0, src);
-        s.kv = __shfl(s.kv, src);
-        splits = __shfl(splits, src);
+        auto from = [&](int32_t v) { return __builtin_amdgcn_readlane(v, src); };
+        if (JOIN) first += from(sum - items);
+        rest -= from(JOIN ? count - tiles : sum - items);
+        s.q0 = from(s.q0);
+        s.n = from(s.n);
+        s.p0 = from(s.p0);
+        s.kv = from(s.kv);
+        it.splits = from(splits);
         it.b = b0 + src;
         break;
       }
-      if (JOIN) first += __shfl(sum, 63);
-      rest -= __shfl(JOIN ? count : sum, 63);
+      if (JOIN) first += __builtin_amdgcn_readlane(sum, 63);
+      rest -= __builtin_amdgcn_readlane(JOIN ? count : sum, 63);
     }
     if (it.b < 0) return it;
   }
-  auto uni = [](int32_t v) { return __builtin_amdgcn_readfirstlane(v); };
-  it.b = uni(it.b);
-  it.splits = uni(splits);
-  const int32_t r = uni((int32_t)rest);
-  it.tile = JOIN ? r : r / it.splits;
-  it.split = JOIN ? 0 : r % it.splits;
-  if (JOIN) *base = first + (int64_t)r * it.splits;
+  const uint32_t r = uni(rest), tile = JOIN ? r : r / it.splits;
+  it.split = JOIN ? 0 : (int32_t)(r - tile * it.splits);
+  if (JOIN) *base = first + r * it.splits;
   it.q0 = uni(s.q0);
   it.n = uni(s.n);
   it.p0 = uni(s.p0);
   it.kv = uni(s.kv);
+  const uint32_t row0 = tile * a.tile_rows;
+  it.rows = min(a.tile_rows, (int32_t)(it.n * a.group - row0));
+  it.tok0 = uni(row0 / a.group);
+  it.head0 = uni(row0 - it.tok0 * a.group);
   return it;
 }
 
@@ -185,16 +186,18 @@ struct Pages {
   int32_t pages;         // valid page numbers are below
   int32_t first;         // entry of lane 0
   int32_t now, next;
+  bool holes;            // a page of `now` is missing
 
   __device__ int32_t load(int32_t at) const {
     const int32_t i = at + (int32_t)(threadIdx.x & 63);
-    const int32_t id = i < count ? table[i] : -1;
-    return id < pages ? id : -1;
+    const int32_t id = i < count ? table[i] : 0;
+    return id >= 0 && id < pages ? id : -1;
   }
   __device__ void begin(int32_t at) {
     first = at;
     now = load(at);
     next = load(at + 64);
+    holes = __ballot(now < 0) != 0;
   }
   // Makes entry `at` (which never decreases) one of `now`'s.
   __device__ void reach(int32_t at) {
@@ -202,47 +205,64 @@ struct Pages {
       first += 64;
       now = next;
       next = load(first + 64);
+      holes = __ballot(now < 0) != 0;
     }
   }
   __device__ int32_t id(int32_t at) const { return __builtin_amdgcn_readlane(now, at - first); }
 };
 
-// Copies of a cache tile: ROWS keys of D elements from key k0 on go to LDS rows of
-// D / 8 chunks of 16 bytes, by NW waves of which this is number wv.  Chunk c of
-// row r is stored at c ^ swizzle: for keys (read as 8 chunks of one column by 8
-// rows) r % 8, for values (read as 4 rows by 2 chunks) 2 (r % 8), or 2 (r % 4) in
-// rows of 8 chunks, so that a read's lanes fall on different banks.
+// Where 16 keys (a multiple of 16 first) lie in the cache, and how many are there:
+// none of a missing page, and none past the end.
+struct Block {
+  int64_t at;    // bytes into k or v
+  int32_t rows;
+};
+
+template <int D>
+__device__ inline Block block_of(const AttnArgs &a, const Pages &pg, int32_t kh, int32_t key, int32_t kv) {
+  const int32_t id = pg.id(key >> a.page_shift);
+  const int32_t in_page = key & (a.o.cache.page - 1);
+  Block b;
+  b.rows = id < 0 ? 0 : min(max(kv - key, 0), 16);
+  b.at = ((int64_t)max(id, 0) * a.head_rows + ((int64_t)kh << a.page_shift) + in_page) * (D * 2);
+  return b;
+}
+
+// Copies of a wave: 16 keys of D elements go to 16 LDS rows of D / 8 chunks of 16
+// bytes, 1 KiB at a time; rows that are not there are zeros.  Chunk c of row r is
+// stored at c ^ swizzle: for keys (read as 8 rows by one chunk) r % 8, for values
+// (read as 4 rows by 2 chunks) 2 (r % 8), or 2 (r % 4) in rows of 8 chunks, so that
+// a read's lanes fall on different banks.  The swizzle repeats every 8 rows, so
+// D / 64 lane offsets serve all copies; one buffer descriptor serves the 16 keys
+// (built for each copy, its 30 scalar instructions took 140 ns of a lone wave, four
+// times what the copy does).
 template <int D>
 __device__ inline uint32_t k_swizzle(uint32_t r) { return r & 7; }
 template <int D>
 __device__ inline uint32_t v_swizzle(uint32_t r) { return (r & (D == 64 ? 3 : 7)) << 1; }
 
-template <int D, int ROWS, int NW, bool V>
+template <int D, bool V>
 struct Copy {
-  static constexpr int kChunks = D / 8;
-  static constexpr int kRows = 64 / kChunks;  // of one wave's copy
-  static constexpr int kCopies = ROWS / kRows / NW;
+  static constexpr int kRows = 512 / D;      // of one copy
+  static constexpr int kCopies = D / 32;     // of 16 keys
+  static constexpr int kOffsets = D / 64;    // copies of 8 rows
+  uint32_t off[kOffsets];
 
-  __device__ static void issue(const uint8_t *cache, int64_t head_rows, int64_t head, int page_shift,
-                               const Pages &pg, int32_t k0, int32_t kv, uint32_t lds, int wv) {
-    const int lane = threadIdx.x & 63;
-    const uint32_t lr = lane / kChunks, lc = lane % kChunks;
+  __device__ void begin() {
+    const uint32_t lane = threadIdx.x & 63, lr = lane / (D / 8), lc = lane % (D / 8);
 #pragma unroll
-    for (int n = 0; n < kCopies; ++n) {
-      const int row0 = (n * NW + wv) * kRows;  // same in all lanes
-      const uint32_t r = row0 + lr;
-      const uint32_t chunk = lc ^ (V ? v_swizzle<D>(r) : k_swizzle<D>(r));
-      const int32_t key = __builtin_amdgcn_readfirstlane(k0 + row0);
-      const int32_t id = pg.id(key >> page_shift);
-      const int32_t in_page = key & ((1 << page_shift) - 1);
-      // rows past the end, and those of a missing page, are zeros
-      const int32_t rows = id < 0 ? 0 : min(max(kv - key, 0), kRows);
-      const int64_t at = ((id < 0 ? 0 : (int64_t)id) * head_rows + head + in_page) * (D * 2);
-      i32x4_t r4 = rsrc4(cache + at, (uint32_t)rows * (D * 2));
-#pragma unroll
-      for (int i = 0; i < 3; ++i) r4[i] = __builtin_amdgcn_readfirstlane(r4[i]);
-      copy_lds(r4, lr * (D * 2) + chunk * 16, lds + (uint32_t)(n * NW + wv) * 1024);
+    for (int i = 0; i < kOffsets; ++i) {
+      const uint32_t r = i * kRows + lr;
+      off[i] = r * (D * 2) + (lc ^ (V ? v_swizzle<D>(r) : k_swizzle<D>(r))) * 16;
     }
+  }
+  __device__ void issue(const void *cache, const Block &b, uint32_t lds) const {
+    i32x4_t r4 = rsrc4(static_cast<const uint8_t *>(cache) + b.at, (uint32_t)b.rows * (D * 2));
+#pragma unroll
+    for (int i = 0; i < 3; ++i) r4[i] = __builtin_amdgcn_readfirstlane(r4[i]);
+#pragma unroll
+    for (int c = 0; c < kCopies; ++c)
+      copy_lds(r4, off[c % kOffsets] + (c / kOffsets) * (8 * D * 2), lds + c * 1024);
   }
 };
 
@@ -250,6 +270,13 @@ template <int N>
 __device__ inline void wait_vm() {
   __builtin_amdgcn_sched_barrier(0);
   asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(N) : "memory");
+  __builtin_amdgcn_sched_barrier(0);
+}
+
+// This wave's reads of LDS have been answered.
+__device__ inline void wait_lds() {
+  __builtin_amdgcn_sched_barrier(0);
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
   __builtin_amdgcn_sched_barrier(0);
 }
 
@@ -517,41 +544,43 @@ __device__ inline float2 *part_ml(const AttnArgs &a, int64_t item, int32_t row, 
 // This workgroup's item and key/value head.  Neighbouring workgroups go to the 8
 // XCDs in turn; each XCD gets a contiguous run of (head, item) so that tiles of
 // one sequence and head, which read the same keys, share its L2.
-__device__ inline void locate(const AttnArgs &a, int32_t &head, int64_t &at) {
+__device__ inline void locate(const AttnArgs &a, int32_t &head, uint32_t &at) {
+  // Single tiles share nothing: in order, the items that exist (the grid is an
+  // upper bound) fall to the XCDs evenly.
   const uint32_t per = (a.grid + kXcds - 1) / kXcds;
-  const uint32_t id = (blockIdx.x % kXcds) * per + blockIdx.x / kXcds;
-  head = (int32_t)(id / a.items);
-  at = id % a.items;
+  const uint32_t id = a.spread ? blockIdx.x : (blockIdx.x % kXcds) * per + blockIdx.x / kXcds;
+  head = (int32_t)(a.spread ? id % a.o.cache.heads : id / a.items);
+  at = a.spread ? id / a.o.cache.heads : id % a.items;
 }
 
 // The row of q / out that row `r` of an item's tile is, or -1.
 __device__ inline int64_t row_of(const AttnArgs &a, const Item &it, int32_t r, int32_t kh, int32_t &tok,
                                  int32_t &head) {
-  const int64_t R = (int64_t)it.tile * a.tile_rows + r;
-  tok = (int32_t)(R / a.group);
-  head = kh * a.group + (int32_t)(R % a.group);
-  return tok < it.n ? (int64_t)it.q0 + tok : -1;
+  const uint32_t at = it.head0 + r, t = at / (uint32_t)a.group;
+  tok = it.tok0 + (int32_t)t;
+  head = kh * a.group + (int32_t)(at - t * a.group);
+  return r < it.rows ? (int64_t)it.q0 + tok : -1;
 }
 
-// Intervals of a wave's rows: each lane's own, and bounds over the lanes.
+// Intervals of a wave's rows r0 .. r0 + 31 of the tile: each lane's own, and
+// bounds over the lanes, which the first and the last row give (a later token's
+// interval neither begins nor ends before an earlier one's).
 template <class W>
-__device__ inline void intervals(const AttnArgs &a, const Item &it, int32_t tok, bool live, W &w) {
+__device__ inline void intervals(const AttnArgs &a, const Item &it, int32_t r0, int32_t tok, bool live, W &w) {
   const int32_t prefix = a.o.prefix ? a.o.prefix[it.b] : 0;
   interval(a, it.p0 + tok, it.kv, prefix, w.lo, w.hi);
   if (!live) w.lo = 0, w.hi = 0x7fffffff;
-  int32_t al = live ? w.lo : 0, ah = live ? w.hi : 0x7fffffff, yl = live ? w.lo : 0x7fffffff,
-          yh = live ? w.hi : 0;
-#pragma unroll
-  for (int d = 16; d >= 1; d >>= 1) {
-    al = max(al, __shfl_xor(al, d));
-    ah = min(ah, __shfl_xor(ah, d));
-    yl = min(yl, __shfl_xor(yl, d));
-    yh = max(yh, __shfl_xor(yh, d));
-  }
-  w.all_lo = __builtin_amdgcn_readfirstlane(al);
-  w.all_hi = __builtin_amdgcn_readfirstlane(ah);
-  w.any_lo = __builtin_amdgcn_readfirstlane(yl);
-  w.any_hi = __builtin_amdgcn_readfirstlane(yh);
+  int32_t first, last, head;
+  row_of(a, it, r0, 0, first, head);
+  row_of(a, it, min(r0 + 31, it.rows - 1), 0, last, head);
+  int32_t fl, fh, ll, lh;
+  interval(a, it.p0 + first, it.kv, prefix, fl, fh);
+  interval(a, it.p0 + last, it.kv, prefix, ll, lh);
+  const bool some = r0 < it.rows;
+  w.any_lo = __builtin_amdgcn_readfirstlane(some ? fl : 0x7fffffff);
+  w.any_hi = __builtin_amdgcn_readfirstlane(some ? lh : 0);
+  w.all_lo = __builtin_amdgcn_readfirstlane(ll);
+  w.all_hi = __builtin_amdgcn_readfirstlane(fh);
 }
 
 // Tiles of BK keys [t0, t1) of a split of [lo, hi).
@@ -565,6 +594,7 @@ __device__ inline void split_range(const Item &it, int32_t lo, int32_t hi, int32
 // Bit s is set where the 16 keys from k0 + 16 s on are on a missing page.
 template <int BK>
 __device__ inline uint32_t missing_of(const Pages &pg, int32_t k0, int32_t kv, int page_shift) {
+  if (!pg.holes) return 0;
   uint32_t bits = 0;
 #pragma unroll
   for (int s = 0; s < BK / 16; ++s)
@@ -580,9 +610,9 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) attn_tile_kernel(AttnAr
   __shared__ __attribute__((aligned(1024))) uint8_t lds[4 * kTile];
   const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   int32_t kh;
-  int64_t at;
+  uint32_t at;
   locate(a, kh, at);
-  if (kh >= a.o.cache.heads) return;
+  if (kh >= a.o.cache.heads || at >= a.items) return;
   const Item it = find_item<false>(a, at);
   if (it.b < 0) return;
 
@@ -593,14 +623,15 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) attn_tile_kernel(AttnAr
   const uint16_t *qrow =
       live ? static_cast<const uint16_t *>(a.o.q) + row * a.o.q_stride + (int64_t)head * D : nullptr;
   load_query<D>(w.q, qrow, a.flip);
-  intervals(a, it, tok, live, w);
+  intervals(a, it, 32 * wv, tok, live, w);
   w.begin();
 
   // keys that any row of the workgroup sees: its first and last token bound them
   int32_t lo, hi, t0, t1;
   {
-    const int32_t first = (int32_t)((int64_t)it.tile * 128 / a.group);
-    const int32_t last = min((int32_t)(((int64_t)it.tile * 128 + 127) / a.group), it.n - 1);
+    int32_t first, last, h;
+    row_of(a, it, 0, 0, first, h);
+    row_of(a, it, it.rows - 1, 0, last, h);
     const int32_t prefix = a.o.prefix ? a.o.prefix[it.b] : 0;
     int32_t x;
     interval(a, it.p0 + first, it.kv, prefix, lo, x);
@@ -611,28 +642,32 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) attn_tile_kernel(AttnAr
   pg.table = a.o.table + (int64_t)it.b * a.o.table_stride;
   pg.count = (it.kv + a.o.cache.page - 1) >> a.page_shift;
   pg.pages = a.o.cache.pages;
-  const int64_t hr = a.head_rows, ho = (int64_t)kh << a.page_shift;
+  const int64_t ho = (int64_t)kh << a.page_shift;
   const uint32_t base = lds_addr(lds);
+  Copy<D, false> kc;
+  Copy<D, true> vc;
+  kc.begin();
+  vc.begin();
+  // 16 keys and values to each wave, or (tiles of 32 keys) 16 keys or 16 values
   auto request = [&](int32_t t) {
     const int32_t k0 = t * BK;
     const uint32_t to = base + (uint32_t)(t & 1) * (2 * kTile);
     pg.reach(k0 >> a.page_shift);
-    Copy<D, BK, 4, false>::issue(static_cast<const uint8_t *>(a.o.cache.k), hr, ho, a.page_shift, pg, k0,
-                                 it.kv, to, wv);
-    Copy<D, BK, 4, true>::issue(static_cast<const uint8_t *>(a.o.cache.v), hr, ho, a.page_shift, pg, k0,
-                                it.kv, to + kTile, wv);
+    const int part = wv % (BK / 16);
+    const Block b = block_of<D>(a, pg, kh, k0 + 16 * part, it.kv);
+    const uint32_t at = to + part * (16 * D * 2);
+    if (BK == 64 || wv < 2) kc.issue(a.o.cache.k, b, at);
+    if (BK == 64 || wv >= 2) vc.issue(a.o.cache.v, b, at + kTile);
     return missing_of<BK>(pg, k0, it.kv, a.page_shift);
   };
   uint32_t gone = 0;
-  if (t0 < t1) {
-    pg.begin((t0 * BK) >> a.page_shift);
-    gone = request(t0);
-  }
-  for (int32_t t = t0; t < t1; ++t) {
+  if (t0 < t1) pg.begin((t0 * BK) >> a.page_shift);
+  for (int32_t t = t0 - 1; t < t1; ++t) {
     // tile t is in LDS, and every wave has done with the tile before it
     wait_vm_barrier<0>();
     const uint32_t missing = gone;
     if (t + 1 < t1) gone = request(t + 1);
+    if (t < t0) continue;
     const int32_t k0 = t * BK;
     if (k0 < w.any_hi && k0 + BK > w.any_lo) {
       const uint8_t *k = lds + (t & 1) * (2 * kTile);
@@ -699,24 +734,30 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) attn_tile_kernel(AttnAr
   }
 }
 
+// Workgroups of the stream kernel on a CU: what its registers (D = 64) or its part of
+// LDS allow.
+template <int D>
+constexpr int kStreamWgs = D == 64 ? 3 : 256 / D;
+
 // Few rows: up to 32, the same for all waves, which take the tiles of 32 keys in
 // turn.  A wave copies its own tiles to its own part of LDS, keys while it works
 // on values and values while it works on keys, and waits for no other wave; the
-// four waves' sums are joined in LDS at the end.
+// four waves' sums are joined in LDS at the end.  Of one tile or few a wave the
+// kernel is a chain of latencies, and fetching code that has not run yet is one of
+// them: the sums are joined in chunks of 16 bytes, a quarter of the code.
 template <int T, int D, bool CAP>
-__global__ void __launch_bounds__(256, 1) attn_stream_kernel(AttnArgs a) {
+__global__ void __launch_bounds__(256, kStreamWgs<D>) attn_stream_kernel(AttnArgs a) {
   constexpr int BK = 32, kTile = BK * D * 2;
-  using K = Copy<D, BK, 1, false>;
-  using V = Copy<D, BK, 1, true>;
+  constexpr int kCopies = 2 * Copy<D, false>::kCopies;  // of a wave's tile of keys, or of values
   static_assert(2 * kTile == 32 * D * 4, "a wave's tiles and its sums take the same room");
   __shared__ __attribute__((aligned(1024))) uint8_t lds[4 * 2 * kTile];
-  __shared__ float ml[2][4][32];
+  __shared__ float2 ml[4][32];
   __shared__ uint32_t again;
   const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   int32_t kh;
-  int64_t at;
+  uint32_t at;
   locate(a, kh, at);
-  if (kh >= a.o.cache.heads) return;
+  if (kh >= a.o.cache.heads || at >= a.items) return;
   const Item it = find_item<false>(a, at);
   if (it.b < 0) return;
 
@@ -728,28 +769,33 @@ __global__ void __launch_bounds__(256, 1) attn_stream_kernel(AttnArgs a) {
   pg.table = a.o.table + (int64_t)it.b * a.o.table_stride;
   pg.count = (it.kv + a.o.cache.page - 1) >> a.page_shift;
   pg.pages = a.o.cache.pages;
-  intervals(a, it, tok, live, w);
+  intervals(a, it, 0, tok, live, w);
   int32_t t0, t1;
   split_range<BK>(it, w.any_lo, w.any_hi, t0, t1);
-  const int64_t hr = a.head_rows, ho = (int64_t)kh << a.page_shift;
+  const int64_t ho = (int64_t)kh << a.page_shift;
   uint8_t *const mine = lds + wv * (2 * kTile);
   const uint32_t to = lds_addr(mine);
-  auto keys = [&](int32_t t) {  // past t1: nothing to read, but the copies count
-    const int32_t k0 = t * BK;
-    if (t < t1) pg.reach(k0 >> a.page_shift);
-    K::issue(static_cast<const uint8_t *>(a.o.cache.k), hr, ho, a.page_shift, pg,
-             t < t1 ? k0 : pg.first << a.page_shift, t < t1 ? it.kv : 0, to, 0);
+  Copy<D, false> kc;
+  Copy<D, true> vc;
+  kc.begin();
+  vc.begin();
+  Block b0, b1;  // the tile whose keys were requested last
+  auto keys = [&](int32_t t) {
+    pg.reach((t * BK) >> a.page_shift);
+    b0 = block_of<D>(a, pg, kh, t * BK, it.kv);
+    b1 = block_of<D>(a, pg, kh, t * BK + 16, it.kv);
+    kc.issue(a.o.cache.k, b0, to);
+    kc.issue(a.o.cache.k, b1, to + kTile / 2);
   };
-  auto values = [&](int32_t t) {
-    const int32_t k0 = t * BK;
-    V::issue(static_cast<const uint8_t *>(a.o.cache.v), hr, ho, a.page_shift, pg,
-             t < t1 ? k0 : pg.first << a.page_shift, t < t1 ? it.kv : 0, to + kTile, 0);
+  auto values = [&] {
+    vc.issue(a.o.cache.v, b0, to + kTile);
+    vc.issue(a.o.cache.v, b1, to + kTile + kTile / 2);
   };
   const int32_t begin = t0 + wv;
   if (begin < t1) {
     pg.begin((begin * BK) >> a.page_shift);
     keys(begin);
-    values(begin);
+    values();
   }
   load_query<D>(w.q, live ? static_cast<const uint16_t *>(a.o.q) + row * a.o.q_stride + (int64_t)head * D
                           : nullptr, a.flip);
@@ -759,74 +805,70 @@ __global__ void __launch_bounds__(256, 1) attn_stream_kernel(AttnArgs a) {
     const uint32_t missing = missing_of<BK>(pg, k0, it.kv, a.page_shift);
     f32x16_t s[1];
     uint32_t p[1][8];
-    wait_vm<V::kCopies>();  // the keys are here
+    wait_vm<kCopies>();  // the keys are here
     w.scores(s, mine);
-    wait_vm<V::kCopies>();  // and read: their room is free
-    keys(t + 4);
+    const bool more = t + 4 < t1;
+    if (more) {
+      wait_lds();  // and read: their room is free
+      keys(t + 4);
+    }
     w.softmax(a, s, p, k0, missing);
-    wait_vm<K::kCopies>();
+    if (more)
+      wait_vm<kCopies>();
+    else
+      wait_vm<0>();
     w.values(p, mine + kTile);
-    wait_vm<K::kCopies>();
-    values(t + 4);
+    if (more) {
+      wait_lds();
+      values();
+    }
   }
-  wait_vm<0>();
   w.l = Wave<T, D, BK, CAP>::row_sum(w.l);
 
-  // The waves' sums, brought to one maximum and added in the waves' order.  Element
-  // d of row r of a wave is at word 32 d + (r + d) % 32 of its part.
+  // The waves' sums, brought to one maximum and added in the waves' order.  Elements
+  // 4 c .. 4 c + 3 of row r of a wave are chunk c ^ (r % 8) of row r of its part.
   const float c = CAP ? 1.f : a.scale2;
   const int r = lane & 31, half = lane >> 5;
-  if (half == 0) ml[0][wv][r] = w.m * c, ml[1][wv][r] = w.l;
+  if (half == 0) ml[wv][r] = make_float2(w.m * c, w.l);
   if (threadIdx.x == 0) again = 0;
-  __syncthreads();
-  float top = ml[0][0][r];
-#pragma unroll
-  for (int v = 1; v < 4; ++v) top = fmaxf(top, ml[0][v][r]);
-  // a NaN score's maximum is left out by fmaxf, its sum is not
-  const float f = w.m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(w.m * c - top);
-  float *const sums = reinterpret_cast<float *>(mine);
+  float4 *const sums = reinterpret_cast<float4 *>(mine) + r * (D / 4);
 #pragma unroll
   for (int b = 0; b < D / 32; ++b)
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      const int d = 32 * b + 8 * (i / 4) + 4 * half + i % 4;
-      sums[32 * d + ((r + d) & 31)] = w.o[b][i] * f;
-    }
+    for (int i = 0; i < 16; i += 4)
+      sums[(8 * b + i / 2 + half) ^ (r & 7)] = make_float4(w.o[b][i], w.o[b][i + 1], w.o[b][i + 2], w.o[b][i + 3]);
   __syncthreads();
   const bool split = it.splits > 1;
   const int64_t item = (int64_t)kh * a.items + at;
-  const float *all = reinterpret_cast<const float *>(lds);
-  const int32_t rows = (int32_t)min((int64_t)32, (int64_t)it.n * a.group - (int64_t)it.tile * 32);
-  for (int32_t e = threadIdx.x; e < rows * (D / 4); e += 256) {
-    const int32_t rr = e / (D / 4), d0 = 4 * (e % (D / 4));
-    float mx = ml[0][0][rr], l = 0.f, v[4];
+  const float4 *all = reinterpret_cast<const float4 *>(lds);
+  for (int32_t e = threadIdx.x; e < it.rows * (D / 4); e += 256) {
+    const int32_t rr = e / (D / 4), ch = e % (D / 4);
+    float mx = -INFINITY, l = 0.f;
 #pragma unroll
-    for (int u = 1; u < 4; ++u) mx = fmaxf(mx, ml[0][u][rr]);
+    for (int u = 0; u < 4; ++u) mx = fmaxf(mx, ml[u][rr].x);
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
-      const float mu = ml[0][u][rr];
-      l += ml[1][u][rr] * (mu == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mu - mx));
+      const float2 x = ml[u][rr];
+      // (a wave that saw nothing has sums of 0, or NaN, which stays)
+      const float f = x.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(x.x - mx);
+      const float4 y = all[u * (8 * D) + rr * (D / 4) + (ch ^ (rr & 7))];
+      l = __builtin_fmaf(x.y, f, l);
+      v.x = __builtin_fmaf(y.x, f, v.x);
+      v.y = __builtin_fmaf(y.y, f, v.y);
+      v.z = __builtin_fmaf(y.z, f, v.z);
+      v.w = __builtin_fmaf(y.w, f, v.w);
     }
-    bool ok = l * 0.f == 0.f;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int d = d0 + j;
-      float x = 0.f;
-#pragma unroll
-      for (int u = 0; u < 4; ++u) x += all[u * (32 * D) + 32 * d + ((rr + d) & 31)];
-      v[j] = x;
-      ok = ok && x * 0.f == 0.f;
-    }
-    if (!ok) atomicOr(&again, 1u << rr);
+    if (!((v.x + v.y + v.z + v.w + l) * 0.f == 0.f)) atomicOr(&again, 1u << rr);
     int32_t tk, hd;
     const int64_t rw = row_of(a, it, rr, kh, tk, hd);
     if (split) {
-      *reinterpret_cast<float4 *>(part_o(a, item, rr, D) + d0) = make_float4(v[0], v[1], v[2], v[3]);
-      if (d0 == 0) *part_ml(a, item, rr, D) = make_float2(mx, l);
+      *reinterpret_cast<float4 *>(part_o(a, item, rr, D) + 4 * ch) = v;
+      if (ch == 0) *part_ml(a, item, rr, D) = make_float2(mx, l);
     } else {
       const float inv = l != 0.f ? 1.f / l : 0.f;
-      *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(a.o.out) + rw * a.o.out_stride + (int64_t)hd * D + d0) =
-          make_uint2(pack2<T>(v[0] * inv, v[1] * inv), pack2<T>(v[2] * inv, v[3] * inv));
+      *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(a.o.out) + rw * a.o.out_stride + (int64_t)hd * D + 4 * ch) =
+          make_uint2(pack2<T>(v.x * inv, v.y * inv), pack2<T>(v.z * inv, v.w * inv));
     }
   }
   __syncthreads();
@@ -857,24 +899,23 @@ __global__ void __launch_bounds__(256, 1) attn_stream_kernel(AttnArgs a) {
 }
 
 // Joins the splits of a tile's rows, in an order that the number of splits decides.
-// D / 4 lanes read a row's sums at once, so a workgroup has 1024 / D places: with
-// few splits each takes a row of its own; with many, all take a part of one row's
-// splits (every 1024 / D-th) and their sums meet in LDS.
+// Up to 16: D / 4 lanes take a row.  More: a workgroup takes 64 elements of a row, 16
+// lanes reading a split's and 16 groups of lanes every 16th split, whose sums meet in
+// LDS; that many requests at once, since what other XCDs wrote comes from behind
+// this one's L2.
 template <int T, int D>
 __global__ void __launch_bounds__(256) attn_join_kernel(AttnArgs a) {
-  constexpr int kLanes = D / 4, kPlaces = 256 / kLanes;
+  constexpr int kLanes = D / 4, kPlaces = 256 / kLanes, kParts = D / 64;
   __shared__ float weight[kMaxSplits];
   __shared__ float red[8];
   __shared__ float4 part[256];
   const int32_t kh = (int32_t)(blockIdx.x / a.tiles);
-  int64_t base;
-  const Item it = find_item<true>(a, blockIdx.x % a.tiles, &base);
-  if (it.b < 0 || it.splits == 1 || it.splits > kMaxSplits || base + it.splits > a.items) return;
-  base += (int64_t)kh * a.items;
-  const int place = threadIdx.x / kLanes, d0 = 4 * (threadIdx.x % kLanes);
-  const int32_t rows =
-      (int32_t)min((int64_t)a.tile_rows, (int64_t)it.n * a.group - (int64_t)it.tile * a.tile_rows);
-  auto store = [&](int32_t r, float4 v, float l) {
+  uint32_t first;
+  const Item it = find_item<true>(a, blockIdx.x % a.tiles, &first);
+  if (it.b < 0 || it.splits <= 1 || it.splits > kMaxSplits || first > a.items || it.splits > a.items - first)
+    return;
+  const int64_t base = (int64_t)kh * a.items + first;
+  auto store = [&](int32_t r, int d0, float4 v, float l) {
     int32_t tok, head;
     const int64_t row = row_of(a, it, r, kh, tok, head);
     const float inv = l != 0.f ? 1.f / l : 0.f;
@@ -887,24 +928,27 @@ __global__ void __launch_bounds__(256) attn_join_kernel(AttnArgs a) {
     v.z = __builtin_fmaf(x.z, f, v.z);
     v.w = __builtin_fmaf(x.w, f, v.w);
   };
-  if (it.splits <= kPlaces) {
-    for (int32_t r = blockIdx.y * kPlaces + place; r < rows; r += gridDim.y * kPlaces) {
+  if (it.splits <= 16) {
+    const int place = threadIdx.x / kLanes, d0 = 4 * (threadIdx.x % kLanes);
+    for (int32_t r = blockIdx.y * kPlaces + place; r < it.rows; r += gridDim.y * kPlaces) {
       float m = -INFINITY, l = 0.f;
+#pragma unroll 8
       for (int32_t s = 0; s < it.splits; ++s) m = fmaxf(m, part_ml(a, base + s, r, D)->x);
       float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
+#pragma unroll 8
       for (int32_t s = 0; s < it.splits; ++s) {
         const float2 ml = *part_ml(a, base + s, r, D);
         const float f = ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml.x - m);
         l = __builtin_fmaf(ml.y, f, l);
         add(v, *reinterpret_cast<const float4 *>(part_o(a, base + s, r, D) + d0), f);
       }
-      store(r, v, l);
+      store(r, d0, v, l);
     }
     return;
   }
-  const int wv = threadIdx.x >> 6;
-  for (int32_t r = blockIdx.y; r < rows; r += gridDim.y) {
+  const int wv = threadIdx.x >> 6, place = threadIdx.x >> 4;
+  const int d0 = 64 * (blockIdx.y % kParts) + 4 * (threadIdx.x & 15);
+  for (int32_t r = blockIdx.y / kParts; r < it.rows; r += gridDim.y / kParts) {
     float m = -INFINITY, l = 0.f;
     for (int32_t s = threadIdx.x; s < it.splits; s += 256) m = fmaxf(m, part_ml(a, base + s, r, D)->x);
 #pragma unroll
@@ -924,15 +968,15 @@ __global__ void __launch_bounds__(256) attn_join_kernel(AttnArgs a) {
     __syncthreads();
     l = (red[4] + red[5]) + (red[6] + red[7]);
     float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 8
-    for (int32_t s = place; s < it.splits; s += kPlaces)
+#pragma unroll 16
+    for (int32_t s = place; s < it.splits; s += 16)
       add(v, *reinterpret_cast<const float4 *>(part_o(a, base + s, r, D) + d0), weight[s]);
     part[threadIdx.x] = v;
     __syncthreads();
     if (place == 0) {
 #pragma unroll
-      for (int q = 1; q < kPlaces; ++q) add(v, part[q * kLanes + threadIdx.x], 1.f);
-      store(r, v, l);
+      for (int q = 1; q < 16; ++q) add(v, part[q * 16 + threadIdx.x], 1.f);
+      store(r, d0, v, l);
     }
     __syncthreads();
   }
@@ -956,11 +1000,11 @@ hipError_t attn_launch_d(const AttnArgs &a, hipStream_t s) {
   }
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.target <= 0) return e;
-  // a workgroup per row, up to 2048 of them
+  // a workgroup per 64 elements of a row, up to 2048 of them
   const uint32_t tiles = a.tiles * (uint32_t)a.o.cache.heads;
   const uint32_t most = tiles >= 2048 ? 1 : 2048 / tiles;
-  attn_join_kernel<T, D>
-      <<<dim3(tiles, (uint32_t)a.part_rows < most ? (uint32_t)a.part_rows : most), 256, 0, s>>>(a);
+  const uint32_t rows = (uint32_t)a.part_rows < most ? (uint32_t)a.part_rows : most;
+  attn_join_kernel<T, D><<<dim3(tiles, rows * (D / 64)), 256, 0, s>>>(a);
   return hipGetLastError();
 }
 

@@ -106,7 +106,8 @@ def test_rope_refusals(eb, kw, status):
     (dict(rows=-1), -1), (dict(batch=0), -1), (dict(batch=4097), -1), (dict(q_heads=0), -1), (dict(q_heads=7), -1),
     (dict(q_heads=4098), -1), (dict(q_stride=1016), -1), (dict(out_stride=1016), -1), (dict(q_stride=1028), -2),
     (dict(out_stride=1026), -2), (dict(table_stride=0), -1), (dict(table_stride=1 << 27), -1),
-    (dict(max_new=0), -1), (dict(max_kv=0), -1), (dict(window=-1), -1), (dict(mask=2), -1),
+    (dict(rows=1 << 24, q_heads=256, q_stride=1 << 15, out_stride=1 << 15), -1), (dict(max_new=0), -1),
+    (dict(max_kv=0), -1), (dict(window=-1), -1), (dict(mask=2), -1),
     (dict(scale=float("inf")), -1), (dict(softcap=-1.0), -1), (dict(softcap=float("nan")), -1), (dict(q=0), -1),
     (dict(out=0), -1), (dict(table=0), -1), (dict(q_start=0), -1), (dict(kv_len=0), -1),
     (dict(q=3 * GB + 2), -2), (dict(out=4 * GB + 8), -2), (dict(prefix=8 * GB + 1), -2), (dict(out=3 * GB), -1),
