@@ -304,9 +304,7 @@ struct Wave {
 
   __device__ void begin() {
 #pragma unroll
-    for (int b = 0; b < kBlocks; ++b)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) o[b][i] = 0.f;
+    for (int b = 0; b < kBlocks; ++b) o[b] = f32x16_t(0.f);
     m = -INFINITY;
     l = 0.f;
     masked = false;
@@ -336,9 +334,7 @@ struct Wave {
     const uint8_t *const base = k + row * (D * 2);
     const uint32_t x = half ^ k_swizzle<D>(row);
 #pragma unroll
-    for (int t = 0; t < kTiles; ++t)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) s[t][i] = 0.f;
+    for (int t = 0; t < kTiles; ++t) s[t] = f32x16_t(0.f);
 #pragma unroll
     for (int c = 0; c < kSteps; ++c)
 #pragma unroll
@@ -386,9 +382,7 @@ struct Wave {
       m = to;
       l *= f;
 #pragma unroll
-      for (int b = 0; b < kBlocks; ++b)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) o[b][i] *= f;
+      for (int b = 0; b < kBlocks; ++b) o[b] *= f;  // whole vectors: by element, the loop would copy them
     }
     const float base = m == -INFINITY ? 0.f : -m * c;
 #pragma unroll
@@ -407,18 +401,17 @@ struct Wave {
     const uint32_t lane = threadIdx.x & 63, half = lane >> 5;
     const uint32_t row = 4 * half + (lane & 15) / 4, quad = lane & 3;
     const uint32_t x = (2 * ((lane >> 4) & 1) + quad / 2) ^ v_swizzle<D>(row);
-    const uint32_t base = lds_addr(v) + row * (D * 2) + (quad & 1) * 8;
+    const uint8_t *const base = v + row * (D * 2) + (quad & 1) * 8;
 #pragma unroll
     for (int c = 0; c < 2 * kTiles; ++c) {
       const uint32_t *w = &p[c / 2][4 * (c % 2)];
       const uint4 pb = make_uint4(w[0], w[1], w[2], w[3]);
 #pragma unroll
       for (int b = 0; b < kBlocks; ++b) {
-        const uint32_t at = base + (16 * c) * (D * 2) + (((4 * b) & ~15) << 4) + ((((4 * b) & 15) ^ x) << 4);
-        auto read = [](uint32_t addr) {
-          return __builtin_bit_cast(
-              uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                         (__attribute__((address_space(3))) s16x4_t *)(uintptr_t)addr));
+        const uint8_t *const at = base + ((((4 * b) & 15) ^ x) << 4) + (16 * c) * (D * 2) + (((4 * b) & ~15) << 4);
+        auto read = [](const uint8_t *p) {
+          return __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                                               (__attribute__((address_space(3))) s16x4_t *)p));
         };
         const uint2 v0 = read(at), v1 = read(at + 8 * (D * 2));
         o[b] = mfma32<T>(make_uint4(v0.x, v0.y, v1.x, v1.y), pb, o[b]);
@@ -587,8 +580,9 @@ __device__ inline void intervals(const AttnArgs &a, const Item &it, int32_t r0, 
 template <int BK>
 __device__ inline void split_range(const Item &it, int32_t lo, int32_t hi, int32_t &t0, int32_t &t1) {
   const int32_t a = lo / BK, b = hi > lo ? (hi + BK - 1) / BK : a;
-  t0 = a + (int32_t)((int64_t)(b - a) * it.split / it.splits);
-  t1 = a + (int32_t)((int64_t)(b - a) * (it.split + 1) / it.splits);
+  // (told to be the same in all lanes, or the loop over them would run on lane masks)
+  t0 = __builtin_amdgcn_readfirstlane(a + (int32_t)((int64_t)(b - a) * it.split / it.splits));
+  t1 = __builtin_amdgcn_readfirstlane(a + (int32_t)((int64_t)(b - a) * (it.split + 1) / it.splits));
 }
 
 // Bit s is set where the 16 keys from k0 + 16 s on are on a missing page.
@@ -661,23 +655,32 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) attn_tile_kernel(AttnAr
     return missing_of<BK>(pg, k0, it.kv, a.page_shift);
   };
   uint32_t gone = 0;
-  if (t0 < t1) pg.begin((t0 * BK) >> a.page_shift);
-  for (int32_t t = t0 - 1; t < t1; ++t) {
+  if (t0 < t1) {
+    pg.begin((t0 * BK) >> a.page_shift);
+    gone = request(t0);
+  }
+  auto next = [&](int32_t t) {
     // tile t is in LDS, and every wave has done with the tile before it
     wait_vm_barrier<0>();
     const uint32_t missing = gone;
     if (t + 1 < t1) gone = request(t + 1);
-    if (t < t0) continue;
-    const int32_t k0 = t * BK;
-    if (k0 < w.any_hi && k0 + BK > w.any_lo) {
-      const uint8_t *k = lds + (t & 1) * (2 * kTile);
-      f32x16_t s[BK / 32];
-      uint32_t p[BK / 32][8];
-      w.scores(s, k);
-      w.softmax(a, s, p, k0, missing);
-      w.values(p, k + kTile);
-    }
+    return missing;
+  };
+  // this wave's tiles, between those that only others need (three loops: sums that a
+  // branch in the loop may or may not change are copied, 64 registers a tile)
+  const int32_t c0 = min(max(w.any_lo / BK, t0), t1), c1 = max(min((w.any_hi + BK - 1) / BK, t1), c0);
+  int32_t t = t0;
+  for (; t < c0; ++t) next(t);
+  for (; t < c1; ++t) {
+    const uint32_t missing = next(t);
+    const uint8_t *k = lds + (t & 1) * (2 * kTile);
+    f32x16_t s[BK / 32];
+    uint32_t p[BK / 32][8];
+    w.scores(s, k);
+    w.softmax(a, s, p, t * BK, missing);
+    w.values(p, k + kTile);
   }
+  for (; t < t1; ++t) next(t);
 
   w.l = Wave<T, D, BK, CAP>::row_sum(w.l);
   const bool split = it.splits > 1;
@@ -947,8 +950,9 @@ __global__ void __launch_bounds__(256) attn_join_kernel(AttnArgs a) {
     return;
   }
   const int wv = threadIdx.x >> 6, place = threadIdx.x >> 4;
-  const int d0 = 64 * (blockIdx.y % kParts) + 4 * (threadIdx.x & 15);
-  for (int32_t r = blockIdx.y / kParts; r < it.rows; r += gridDim.y / kParts) {
+  for (int32_t u = blockIdx.y; u < it.rows * kParts; u += gridDim.y) {
+    const int32_t r = u / kParts;
+    const int d0 = 64 * (u % kParts) + 4 * (threadIdx.x & 15);
     float m = -INFINITY, l = 0.f;
     for (int32_t s = threadIdx.x; s < it.splits; s += 256) m = fmaxf(m, part_ml(a, base + s, r, D)->x);
 #pragma unroll
@@ -968,9 +972,17 @@ __global__ void __launch_bounds__(256) attn_join_kernel(AttnArgs a) {
     __syncthreads();
     l = (red[4] + red[5]) + (red[6] + red[7]);
     float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 16
-    for (int32_t s = place; s < it.splits; s += 16)
-      add(v, *reinterpret_cast<const float4 *>(part_o(a, base + s, r, D) + d0), weight[s]);
+    for (int32_t s0 = place; s0 < it.splits; s0 += 16 * 8) {
+      float4 x[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int32_t s = min(s0 + 16 * i, it.splits - 1);
+        x[i] = *reinterpret_cast<const float4 *>(part_o(a, base + s, r, D) + d0);
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (s0 + 16 * i < it.splits) add(v, x[i], weight[s0 + 16 * i]);
+    }
     part[threadIdx.x] = v;
     __syncthreads();
     if (place == 0) {
@@ -1000,11 +1012,12 @@ hipError_t attn_launch_d(const AttnArgs &a, hipStream_t s) {
   }
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.target <= 0) return e;
-  // a workgroup per 64 elements of a row, up to 2048 of them
-  const uint32_t tiles = a.tiles * (uint32_t)a.o.cache.heads;
-  const uint32_t most = tiles >= 2048 ? 1 : 2048 / tiles;
-  const uint32_t rows = (uint32_t)a.part_rows < most ? (uint32_t)a.part_rows : most;
-  attn_join_kernel<T, D><<<dim3(tiles, rows * (D / 64)), 256, 0, s>>>(a);
+  // one workgroup for each 1024 / D rows, or, of few tiles, up to one for each 64
+  // elements of a row
+  const uint32_t tiles = a.tiles * (uint32_t)a.o.cache.heads, rows = (uint32_t)a.part_rows;
+  const uint32_t least = (rows * D + 1023) / 1024, most = 512 / tiles, parts = rows * (D / 64);
+  const uint32_t spare = parts < most ? parts : most;
+  attn_join_kernel<T, D><<<dim3(tiles, least > spare ? least : spare), 256, 0, s>>>(a);
   return hipGetLastError();
 }
 
