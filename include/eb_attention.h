@@ -84,7 +84,7 @@ typedef struct {
   int32_t page;              /* as in eb_kv_cache */
   int32_t pages;
   int32_t table_stride;      /* >= 1, table_stride * page <= 2^30 */
-  int32_t free_capacity;     /* >= 0 */
+  int32_t free_capacity;     /* 0 .. 2^27 */
 } eb_kv_extend_op;
 
 /* EB_ERR_INVALID: null pointer (free_pages may be null with free_capacity 0,

@@ -60,7 +60,7 @@ int64_t row_bytes(int64_t rows, int64_t stride, int64_t width, int64_t size) {
 eb_status check_extend(const eb_kv_extend_op &o) {
   if (o.batch < 1 || o.batch > kMaxBatch || o.rows < 0 || o.rows > kMaxRows || !pow2_page(o.page) ||
       o.pages < 1 || (int64_t)o.pages * o.page > kMaxInt || o.table_stride < 1 ||
-      (int64_t)o.table_stride * o.page > kMaxKeys || o.free_capacity < 0)
+      (int64_t)o.table_stride * o.page > kMaxKeys || o.free_capacity < 0 || o.free_capacity > 1 << 27)
     return EB_ERR_INVALID;
   if (!o.cached || !o.added || !o.table || !o.n_free || !o.n_free_out || !o.q_start || !o.kv_len ||
       !o.short_rows || (o.free_capacity > 0 && !o.free_pages) || (o.rows > 0 && (!o.slots || !o.positions)))

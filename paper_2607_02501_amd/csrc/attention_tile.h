@@ -934,16 +934,28 @@ __global__ void __launch_bounds__(256) attn_join_kernel(AttnArgs a) {
   if (it.splits <= 16) {
     const int place = threadIdx.x / kLanes, d0 = 4 * (threadIdx.x % kLanes);
     for (int32_t r = blockIdx.y * kPlaces + place; r < it.rows; r += gridDim.y * kPlaces) {
+      // all requests at once, those past the last split repeating it and left out
+      float2 ml[16];
       float m = -INFINITY, l = 0.f;
-#pragma unroll 8
-      for (int32_t s = 0; s < it.splits; ++s) m = fmaxf(m, part_ml(a, base + s, r, D)->x);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) ml[i] = *part_ml(a, base + min(i, it.splits - 1), r, D);
       float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 8
-      for (int32_t s = 0; s < it.splits; ++s) {
-        const float2 ml = *part_ml(a, base + s, r, D);
-        const float f = ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml.x - m);
-        l = __builtin_fmaf(ml.y, f, l);
-        add(v, *reinterpret_cast<const float4 *>(part_o(a, base + s, r, D) + d0), f);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) m = fmaxf(m, ml[i].x);
+#pragma unroll
+      for (int s0 = 0; s0 < 16; s0 += 8) {
+        if (s0 >= it.splits) break;
+        float4 x[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          x[i] = *reinterpret_cast<const float4 *>(part_o(a, base + min(s0 + i, it.splits - 1), r, D) + d0);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          if (s0 + i >= it.splits) continue;
+          const float f = ml[s0 + i].x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml[s0 + i].x - m);
+          l = __builtin_fmaf(ml[s0 + i].y, f, l);
+          add(v, x[i], f);
+        }
       }
       store(r, d0, v, l);
     }

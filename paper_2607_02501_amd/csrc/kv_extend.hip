@@ -11,7 +11,7 @@
 // that begins a page writes the table's entry for it.  So no workgroup waits
 // for another, and pages taken in this call are read from the stack, never
 // from table entries that another workgroup writes.  The work is latency: one
-// read of the lengths, 12 scan steps per 256 sequences, a binary search in LDS
+// read of the lengths, 9 scan steps per 512 sequences, a binary search in LDS
 // per row and one dependent read of the page.
 #include <hip/hip_runtime.h>
 
@@ -20,68 +20,77 @@
 namespace eb {
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 512;
+constexpr int32_t kMost = 1 << 30;  // sums stop here: past any number of rows or pages
 
 __device__ inline int64_t nonneg(int32_t v) { return v > 0 ? v : 0; }
+__device__ inline int32_t add_most(int32_t a, int32_t b) { return min(a + b, kMost); }
 
-// Inclusive sum over the workgroup's threads; *total is the sum of all.
-__device__ inline int64_t block_scan(int64_t v, int64_t *red, int64_t *total) {
+// Inclusive sums (rows, pages), each at most kMost, over the workgroup's threads;
+// *total is that of all.
+__device__ inline int2 block_scan(int2 v, int2 *red, int2 *total) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
 #pragma unroll
   for (int d = 1; d < 64; d <<= 1) {
-    const int64_t u = __shfl_up(v, d);
-    if (lane >= d) v += u;
+    const int32_t x = __shfl_up(v.x, d), y = __shfl_up(v.y, d);
+    if (lane >= d) v = make_int2(add_most(v.x, x), add_most(v.y, y));
   }
   if (lane == 63) red[wave] = v;
   __syncthreads();
-  int64_t before = 0, all = 0;
+  int2 before = make_int2(0, 0), all = make_int2(0, 0);
 #pragma unroll
   for (int w = 0; w < kThreads / 64; ++w) {
-    if (w < wave) before += red[w];
-    all += red[w];
+    const int2 u = red[w];
+    if (w < wave) before = make_int2(add_most(before.x, u.x), add_most(before.y, u.y));
+    all = make_int2(add_most(all.x, u.x), add_most(all.y, u.y));
   }
-  __syncthreads();
   *total = all;
-  return v + before;
+  return make_int2(add_most(v.x, before.x), add_most(v.y, before.y));
 }
 
 __global__ void __launch_bounds__(kThreads) kv_extend_kernel(eb_kv_extend_op o, int page_shift) {
   extern __shared__ int32_t lds[];
   int32_t *start = lds;                // [batch + 1], at most o.rows
-  int32_t *taken = lds + o.batch + 1;  // [batch + 1], at most 2^31 - 1
-  __shared__ int64_t red[kThreads / 64];
+  int32_t *taken = lds + o.batch + 1;  // [batch + 1], at most kMost
+  int32_t *cached = taken + o.batch + 1;
+  __shared__ int2 red[2][kThreads / 64];
+  __shared__ int64_t lost;
   const int32_t page = o.page;
   const int64_t capacity = (int64_t)o.table_stride << page_shift;  // tokens of a table row
   const bool first = blockIdx.x == 0;
-  const int64_t n_free = min(nonneg(o.n_free[0]), (int64_t)o.free_capacity);
+  const int32_t n_free = min(max(o.n_free[0], 0), o.free_capacity);
 
-  int64_t rows_before = 0, pages_before = 0;
+  int2 before = make_int2(0, 0);
   for (int32_t b0 = 0; b0 < o.batch; b0 += kThreads) {
     const int32_t b = b0 + (int32_t)threadIdx.x;
     const bool ok = b < o.batch;
     const int64_t have = ok ? nonneg(o.cached[b]) : 0, add = ok ? nonneg(o.added[b]) : 0;
     const int64_t total = min(have + add, capacity), held = (min(have, capacity) + page - 1) >> page_shift;
-    const int64_t need = ok ? ((total + page - 1) >> page_shift) - held : 0;
-    int64_t rows_all, pages_all;
-    const int64_t rows_in = block_scan(add, red, &rows_all);
-    const int64_t pages_in = block_scan(need, red, &pages_all);
+    const int32_t need = ok ? (int32_t)(((total + page - 1) >> page_shift) - held) : 0;
+    const int32_t rows = (int32_t)min(add, (int64_t)o.rows + 1);
+    int2 all;
+    // (the two halves of red in turn: one barrier a chunk of sequences)
+    const int2 in = block_scan(make_int2(rows, need), red[(b0 / kThreads) & 1], &all);
     if (ok) {
-      start[b] = (int32_t)min(rows_before + rows_in - add, (int64_t)o.rows);
-      taken[b] = (int32_t)min(pages_before + pages_in - need, (int64_t)0x7fffffff);
+      // (rows <= 2^24 + 1 and need <= 2^26 of a sequence, so a sum that stopped at kMost
+      // less its own part is still past every row and every page of the stack)
+      start[b] = min(add_most(before.x, in.x - rows), o.rows);
+      taken[b] = add_most(before.y, in.y - need);
+      cached[b] = (int32_t)have;
       if (first) {
         o.q_start[b] = start[b];
         o.kv_len[b] = (int32_t)total;
       }
     }
-    rows_before += rows_all;
-    pages_before += pages_all;
+    before = make_int2(add_most(before.x, all.x), add_most(before.y, all.y));
   }
   if (threadIdx.x == 0) {
-    start[o.batch] = (int32_t)min(rows_before, (int64_t)o.rows);
-    taken[o.batch] = (int32_t)min(pages_before, (int64_t)0x7fffffff);
+    start[o.batch] = min(before.x, o.rows);
+    taken[o.batch] = before.y;
+    lost = 0;
     if (first) {
       o.q_start[o.batch] = start[o.batch];
-      o.n_free_out[0] = (int32_t)max(n_free - pages_before, (int64_t)0);
+      o.n_free_out[0] = max(n_free - before.y, 0);
     }
   }
   __syncthreads();
@@ -107,7 +116,7 @@ __global__ void __launch_bounds__(kThreads) kv_extend_kernel(eb_kv_extend_op o, 
     int32_t slot = -1, pos = 0;
     if (r < live) {
       const int32_t b = find(start, (int32_t)r);
-      const int64_t have = nonneg(o.cached[b]), p = have + r - start[b];
+      const int64_t have = cached[b], p = have + r - start[b];
       pos = (int32_t)min(p, (int64_t)0x7fffffff);
       if (p < capacity) {
         const int64_t held = (have + page - 1) >> page_shift, at = p >> page_shift;
@@ -132,26 +141,28 @@ __global__ void __launch_bounds__(kThreads) kv_extend_kernel(eb_kv_extend_op o, 
   // pages whose entry in the stack is no page.
   int64_t miss = 0;
   for (int32_t b = threadIdx.x; b < o.batch; b += kThreads) {
-    const int64_t have = nonneg(o.cached[b]), all = have + nonneg(o.added[b]);
-    const int64_t total = min(all, capacity);
+    const int64_t have = cached[b], all = have + nonneg(o.added[b]), total = min(all, capacity);
     miss += max(all - max(have, capacity), (int64_t)0);
     const int64_t held = (min(have, capacity) + page - 1) >> page_shift;
     const int64_t end = min(total, held << page_shift);
     if (have < end && valid(o.table[(int64_t)b * o.table_stride + held - 1]) < 0) miss += end - have;
-    const int64_t got = max(n_free - taken[b], (int64_t)0);
+    const int64_t got = max(n_free - taken[b], 0);
     miss += max(total - max(have, (held + got) << page_shift), (int64_t)0);
   }
-  const int32_t took = (int32_t)min((int64_t)taken[o.batch], n_free);
+  const int32_t took = min(taken[o.batch], n_free);
   for (int32_t i = threadIdx.x; i < took; i += kThreads) {
     if (fresh(i) >= 0) continue;
     const int32_t b = find(taken, i);
-    const int64_t have = nonneg(o.cached[b]), total = min(have + nonneg(o.added[b]), capacity);
+    const int64_t have = cached[b], total = min(have + nonneg(o.added[b]), capacity);
     const int64_t at = ((have + page - 1) >> page_shift) + i - taken[b];
     miss += min((at + 1) << page_shift, total) - (at << page_shift);
   }
-  int64_t all;
-  block_scan(miss, red, &all);
-  if (threadIdx.x == 0) o.short_rows[0] = (int32_t)min(all, (int64_t)0x7fffffff);
+#pragma unroll
+  for (int d = 32; d >= 1; d >>= 1) miss += __shfl_xor(miss, d);
+  if ((threadIdx.x & 63) == 0 && miss > 0)
+    atomicAdd(reinterpret_cast<unsigned long long *>(&lost), (unsigned long long)miss);
+  __syncthreads();
+  if (threadIdx.x == 0) o.short_rows[0] = (int32_t)min(lost, (int64_t)0x7fffffff);
 }
 
 }  // namespace
@@ -161,7 +172,7 @@ hipError_t launch_kv_extend(const eb_kv_extend_op &o, hipStream_t s) {
   // a row per thread up to 2 workgroups per CU's worth of rows, then several
   const int64_t wgs = ((int64_t)o.rows + kThreads - 1) / kThreads;
   const unsigned grid = (unsigned)(wgs < 1 ? 1 : (wgs > 512 ? 512 : wgs));
-  const size_t lds = sizeof(int32_t) * 2 * (size_t)(o.batch + 1);
+  const size_t lds = sizeof(int32_t) * 3 * (size_t)(o.batch + 1);
   kv_extend_kernel<<<grid, kThreads, lds, s>>>(o, shift);
   return hipGetLastError();
 }

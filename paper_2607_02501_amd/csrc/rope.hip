@@ -28,43 +28,72 @@ namespace {
 constexpr int kThreads = 256;
 constexpr double kInvTwoPi = 0.15915494309189533577;
 
-// Four elements from e on, as fp32.
-template <int IT>
-__device__ inline float4 load4(const void *p, int64_t e) {
-  if (IT == EB_F32) return *reinterpret_cast<const float4 *>(static_cast<const float *>(p) + e);
-  const ushort4 u = *reinterpret_cast<const ushort4 *>(static_cast<const uint16_t *>(p) + e);
-  return make_float4(from_y16(u.x, IT), from_y16(u.y, IT), from_y16(u.z, IT), from_y16(u.w, IT));
+// Eight elements of a lane as they lie in memory: 4 from e0 on and 4 from e1 on, or
+// (JOINED) 8 from e0 on.
+template <int IT, bool JOINED>
+struct Raw {
+  static constexpr int kWords = IT == EB_F32 ? 8 : 4;
+  uint32_t w[kWords];
+
+  __device__ void load(const char *p, int e0, int e1) {
+    constexpr int kSize = IT == EB_F32 ? 4 : 2;
+    if (IT == EB_F32) {
+      *reinterpret_cast<uint4 *>(w) = *reinterpret_cast<const uint4 *>(p + e0 * kSize);
+      *reinterpret_cast<uint4 *>(w + 4 % kWords) =
+          *reinterpret_cast<const uint4 *>(p + (JOINED ? e0 + 4 : e1) * kSize);
+    } else if (JOINED) {
+      *reinterpret_cast<uint4 *>(w) = *reinterpret_cast<const uint4 *>(p + e0 * kSize);
+    } else {
+      *reinterpret_cast<uint2 *>(w) = *reinterpret_cast<const uint2 *>(p + e0 * kSize);
+      *reinterpret_cast<uint2 *>(w + 2) = *reinterpret_cast<const uint2 *>(p + e1 * kSize);
+    }
+  }
+  __device__ float at(int i) const {
+    if (IT == EB_F32) return __builtin_bit_cast(float, w[i % kWords]);
+    return from_y16((uint16_t)(w[i / 2 % kWords] >> (16 * (i & 1))), IT);
+  }
+};
+
+template <int CT, bool JOINED>
+__device__ inline void store8(uint16_t *p, int e0, int e1, const float (&v)[8]) {
+  uint32_t w[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    w[i] = (uint32_t)to_y16(v[2 * i], CT) | (uint32_t)to_y16(v[2 * i + 1], CT) << 16;
+  if (JOINED) {
+    *reinterpret_cast<uint4 *>(p + e0) = make_uint4(w[0], w[1], w[2], w[3]);
+  } else {
+    *reinterpret_cast<uint2 *>(p + e0) = make_uint2(w[0], w[1]);
+    *reinterpret_cast<uint2 *>(p + e1) = make_uint2(w[2], w[3]);
+  }
 }
 
-template <int CT>
-__device__ inline void store4(uint16_t *p, const float (&v)[4]) {
-  ushort4 u;
-  u.x = to_y16(v[0], CT);
-  u.y = to_y16(v[1], CT);
-  u.z = to_y16(v[2], CT);
-  u.w = to_y16(v[3], CT);
-  *reinterpret_cast<ushort4 *>(p) = u;
-}
-
-template <int IT, int CT, int D>
+// ADJ: adjacent pairs, or nothing rotated: a lane's 8 elements lie together.
+template <int IT, int CT, int D, bool ADJ>
 __global__ void __launch_bounds__(kThreads)
     rope_append_kernel(eb_rope_append_op o, int page_shift, int parts) {
   constexpr int kLanes = D / 8;         // of a head
   constexpr int kHeads = 64 / kLanes;   // of a wave at a time
   const int lane = threadIdx.x & 63, sub = lane % kLanes;
-  const int64_t wave = (int64_t)blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6);
-  const int64_t row = wave / parts;
-  const int part = (int)(wave - row * parts);
+  const uint32_t wave = blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6);
+  const int64_t row = __builtin_amdgcn_readfirstlane(wave / (uint32_t)parts);
+  const int part = __builtin_amdgcn_readfirstlane(wave % (uint32_t)parts);
   if (row >= o.rows) return;
   const int32_t slot = o.slots[row];
-  const int32_t at = slot >> page_shift;
-  if (slot < 0 || at >= o.cache.pages) return;
+  const char *const src = static_cast<const char *>(o.qkv) + row * o.qkv_stride * (IT == EB_F32 ? 4 : 2);
+  const int heads = o.q_heads + 2 * o.cache.heads;
 
   // elements of this lane: 4 from e0 on and 4 from e1 on
   const int half = o.rot / 2, pair = 4 * sub;
-  const bool rotated = pair < half, split = rotated && o.style == EB_ROT_HALF;
+  const bool rotated = pair < half, split = !ADJ && rotated;
   const int e0 = split ? pair : 2 * pair;
   const int e1 = split ? half + pair : 2 * pair + 4;
+  // one step ahead of its use: the next heads' elements
+  const int step = parts * kHeads;
+  int h = part * kHeads + lane / kLanes;
+  Raw<IT, ADJ> next;
+  next.load(src, min(h, heads - 1) * D + e0, min(h, heads - 1) * D + e1);
+
   float cs[4] = {1.f, 1.f, 1.f, 1.f}, sn[4] = {0.f, 0.f, 0.f, 0.f};
   if (rotated) {
 #pragma unroll
@@ -76,68 +105,69 @@ __global__ void __launch_bounds__(kThreads)
       sincospif(2.0f * (float)(turn - __builtin_rint(turn)), &sn[j], &cs[j]);
     }
   }
-  const char *src = static_cast<const char *>(o.qkv) + row * o.qkv_stride * (IT == EB_F32 ? 4 : 2);
-  const int heads = o.q_heads + 2 * o.cache.heads;
-  const int64_t in_page = slot & (o.cache.page - 1);
-  const float4 one = make_float4(1.f, 1.f, 1.f, 1.f);
-  float4 gq0 = one, gq1 = one, gk0 = one, gk1 = one;
+  float gq[8], gk[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) gq[j] = gk[j] = 1.f;
   if (o.q_norm) {
-    gq0 = *reinterpret_cast<const float4 *>(o.q_norm + e0);
-    gq1 = *reinterpret_cast<const float4 *>(o.q_norm + e1);
+    *reinterpret_cast<float4 *>(gq) = *reinterpret_cast<const float4 *>(o.q_norm + e0);
+    *reinterpret_cast<float4 *>(gq + 4) = *reinterpret_cast<const float4 *>(o.q_norm + e1);
   }
   if (o.k_norm) {
-    gk0 = *reinterpret_cast<const float4 *>(o.k_norm + e0);
-    gk1 = *reinterpret_cast<const float4 *>(o.k_norm + e1);
+    *reinterpret_cast<float4 *>(gk) = *reinterpret_cast<const float4 *>(o.k_norm + e0);
+    *reinterpret_cast<float4 *>(gk + 4) = *reinterpret_cast<const float4 *>(o.k_norm + e1);
   }
-#pragma unroll 2
-  for (int h0 = part * kHeads; h0 < heads; h0 += parts * kHeads) {
-    const int h = h0 + lane / kLanes;
-    const bool ok = h < heads;
-    const int64_t in = (int64_t)(ok ? h : heads - 1) * D;
-    const float4 a = load4<IT>(src, in + e0), b = load4<IT>(src, in + e1);
+  const int32_t at = slot >> page_shift;
+  if (slot < 0 || at >= o.cache.pages) return;
+  uint16_t *const q_out = static_cast<uint16_t *>(o.q_out) + row * o.q_stride;
+  const int64_t cell = (((int64_t)at * o.cache.heads) << page_shift) + (slot & (o.cache.page - 1));
+
+  for (int h0 = part * kHeads; h0 < heads; h0 += step, h += step) {
+    float x[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[j] = next.at(j);
+    if (h0 + step < heads)
+      next.load(src, min(h + step, heads - 1) * D + e0, min(h + step, heads - 1) * D + e1);
     const bool is_q = h < o.q_heads, is_v = h >= o.q_heads + o.cache.heads;
-    float x[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-    float ss = 0.f;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) ss = __builtin_fmaf(x[j], x[j], ss);
-#pragma unroll
-    for (int d = kLanes / 2; d >= 1; d >>= 1) ss += __shfl_xor(ss, d);
     if (is_q ? o.q_norm != nullptr : (!is_v && o.k_norm != nullptr)) {
-      const float r = 1.0f / __builtin_sqrtf(ss * (1.0f / D) + o.norm_eps);
-      const float4 g0 = is_q ? gq0 : gk0, g1 = is_q ? gq1 : gk1;
-      const float g[8] = {g0.x, g0.y, g0.z, g0.w, g1.x, g1.y, g1.z, g1.w};
+      float ss = 0.f;
 #pragma unroll
-      for (int j = 0; j < 8; ++j) x[j] = x[j] * r * g[j];
+      for (int j = 0; j < 8; ++j) ss = __builtin_fmaf(x[j], x[j], ss);
+      // (a head's lanes take this branch together)
+#pragma unroll
+      for (int d = kLanes / 2; d >= 1; d >>= 1) ss += __shfl_xor(ss, d);
+      // 1 / sqrt to one step of fp32; its argument kept out of the subnormals
+      const float r = __builtin_amdgcn_rsqf(fmaxf(__builtin_fmaf(ss, 1.0f / D, o.norm_eps), 1.17549435e-38f));
+#pragma unroll
+      for (int j = 0; j < 8; ++j) x[j] = x[j] * r * (is_q ? gq[j] : gk[j]);
     }
     if (rotated && !is_v) {
-      float y[8];
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        // halves: x[j] and x[4 + j]; adjacent: x[2 j] and x[2 j + 1]
-        const float p = split ? x[j] : x[2 * j], q = split ? x[4 + j] : x[2 * j + 1];
-        const float u = p * cs[j] - q * sn[j], v = q * cs[j] + p * sn[j];
-        y[j] = u;
-        y[4 + j] = v;
-      }
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        x[j] = split ? y[j] : (j & 1 ? y[4 + j / 2] : y[j / 2]);
-        x[4 + j] = split ? y[4 + j] : (j & 1 ? y[6 + j / 2] : y[2 + j / 2]);
+        float &a = x[ADJ ? 2 * j : j], &b = x[ADJ ? 2 * j + 1 : 4 + j];
+        const float u = a * cs[j] - b * sn[j], v = b * cs[j] + a * sn[j];
+        a = u;
+        b = v;
       }
     }
-    if (!ok) continue;
+    if (h >= heads) continue;
     uint16_t *dst;
     if (is_q) {
-      dst = static_cast<uint16_t *>(o.q_out) + row * o.q_stride + (int64_t)h * D;
+      dst = q_out + h * D;
     } else {
       const int kh = h - o.q_heads - (is_v ? o.cache.heads : 0);
-      dst = static_cast<uint16_t *>(is_v ? o.cache.v : o.cache.k) +
-            ((((int64_t)at * o.cache.heads + kh) << page_shift) + in_page) * D;
+      dst = static_cast<uint16_t *>(is_v ? o.cache.v : o.cache.k) + (cell + ((int64_t)kh << page_shift)) * D;
     }
-    const float lo[4] = {x[0], x[1], x[2], x[3]}, hi[4] = {x[4], x[5], x[6], x[7]};
-    store4<CT>(dst + e0, lo);
-    store4<CT>(dst + e1, hi);
+    store8<CT, ADJ>(dst, e0, e1, x);
   }
+}
+
+template <int IT, int CT, int D>
+hipError_t launch_style(const eb_rope_append_op &o, int shift, int parts, unsigned grid, hipStream_t s) {
+  if (o.style == EB_ROT_ADJACENT || o.rot == 0)
+    rope_append_kernel<IT, CT, D, true><<<grid, kThreads, 0, s>>>(o, shift, parts);
+  else
+    rope_append_kernel<IT, CT, D, false><<<grid, kThreads, 0, s>>>(o, shift, parts);
+  return hipGetLastError();
 }
 
 template <int IT, int CT>
@@ -149,13 +179,11 @@ hipError_t launch_d(const eb_rope_append_op &o, hipStream_t s) {
   parts = parts < steps ? parts : steps;
   const int64_t waves = o.rows * parts;
   const unsigned grid = (unsigned)((waves + kThreads / 64 - 1) / (kThreads / 64));
-  if (o.cache.dim == 64)
-    rope_append_kernel<IT, CT, 64><<<grid, kThreads, 0, s>>>(o, shift, (int)parts);
-  else if (o.cache.dim == 128)
-    rope_append_kernel<IT, CT, 128><<<grid, kThreads, 0, s>>>(o, shift, (int)parts);
-  else
-    rope_append_kernel<IT, CT, 256><<<grid, kThreads, 0, s>>>(o, shift, (int)parts);
-  return hipGetLastError();
+  switch (o.cache.dim) {
+    case 64: return launch_style<IT, CT, 64>(o, shift, (int)parts, grid, s);
+    case 128: return launch_style<IT, CT, 128>(o, shift, (int)parts, grid, s);
+    default: return launch_style<IT, CT, 256>(o, shift, (int)parts, grid, s);
+  }
 }
 
 }  // namespace

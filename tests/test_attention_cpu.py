@@ -76,7 +76,7 @@ BAD_CACHE = [(dict(cache_k=0), -1), (dict(cache_v=0), -1), (dict(cache_k=GB + 8)
 @pytest.mark.parametrize("kw,status", [
     (dict(batch=0), -1), (dict(batch=4097), -1), (dict(rows=-1), -1), (dict(rows=(1 << 24) + 1), -1),
     (dict(page=12), -1), (dict(page=0), -1), (dict(pages=0), -1), (dict(pages=1 << 27), -1),
-    (dict(table_stride=0), -1), (dict(table_stride=1 << 27), -1), (dict(free_capacity=-1), -1),
+    (dict(table_stride=0), -1), (dict(table_stride=1 << 27), -1), (dict(free_capacity=-1), -1), (dict(free_capacity=(1 << 27) + 1), -1),
     (dict(cached=0), -1), (dict(added=0), -1), (dict(table=0), -1), (dict(free_pages=0), -1),
     (dict(n_free=0), -1), (dict(n_free_out=0), -1), (dict(q_start=0), -1), (dict(kv_len=0), -1),
     (dict(slots=0), -1), (dict(positions=0), -1), (dict(short_rows=0), -1), (dict(table=3 * GB + 2), -2),
