@@ -44,7 +44,11 @@ AttnArgs plan(const eb_attention_op &o) {
   const int64_t slots = cus * (o.cache.dim == 256 ? 1 : o.cache.dim == 64 && a.tile_rows == 32 ? 3 : 2);
   a.unit = a.tile_rows == 32 ? 128 : 64;
   a.min_units = a.tile_rows == 32 ? 1 : 16;
-  if (o.max_kv > a.unit * a.min_units && (o.batch > 1 || tiles * heads * 2 <= slots)) {
+  int64_t see = o.max_kv;
+  if (o.window > 0 && o.mask != EB_MASK_FULL && !o.prefix && see > (int64_t)o.window + a.tile_rows)
+    see = (int64_t)o.window + a.tile_rows;
+  const int64_t units = (see + a.unit - 1) / a.unit;
+  if (tiles * heads * 2 <= slots ? units > a.min_units : o.batch > 1 && units > 16) {
     const int64_t target = (slots + heads - 1) / heads;
     a.target = (int32_t)(target < kMaxSplits ? target : kMaxSplits);
   }
