@@ -34,7 +34,9 @@ COMMON = ["-O3", "-std=c++17", "-fPIC", f"--offload-arch={ARCH}", "-I", INCLUDE,
 PER_FILE = {"quantize.hip": ["-ffp-contract=off"],
             # keep MFMA results in VGPRs where the VALU scales them at once
             "mfma_rows_q8_0.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
-            "mfma_rows_q4_0.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]}
+            "mfma_rows_q4_0.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
+            "attention_bf16.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
+            "attention_f16.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]}
 
 
 def hipcc() -> str:

@@ -160,7 +160,10 @@ __device__ inline Item find_item(const AttnArgs &a, uint32_t at, uint32_t *base 
   it.n = uni(s.n);
   it.p0 = uni(s.p0);
   it.kv = uni(s.kv);
-  const uint32_t row0 = tile * a.tile_rows;
+  // Under a causal mask the last tile of one sequence sees most keys and begins first
+  // (4096 x 4096, 24 heads: 157 -> 134 us; in ragged batches it cost 2 us of 18).
+  const uint32_t tiles = uni(s.tiles);
+  const uint32_t row0 = (o.batch > 1 || o.mask == EB_MASK_FULL ? tile : tiles - 1 - tile) * a.tile_rows;
   it.rows = min(a.tile_rows, (int32_t)(it.n * a.group - row0));
   it.tok0 = uni(row0 / a.group);
   it.head0 = uni(row0 - it.tok0 * a.group);
@@ -288,6 +291,13 @@ __device__ inline uint32_t lds_addr(const void *p) {
 // one wave's 32 rows
 // ---------------------------------------------------------------------------
 
+// Transposing LDS read: with 8 bytes at p from each lane, lane l of 16 gets element
+// l % 4 of the four lanes 4 j + l / 4, j = 0 .. 3.
+__device__ inline uint2 read_tr(const uint8_t *p) {
+  return __builtin_bit_cast(
+      uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t *)p));
+}
+
 template <int T, int D, int BK, bool CAP>
 struct Wave {
   static constexpr int kSteps = D / 16;   // of a score's contraction
@@ -328,37 +338,80 @@ struct Wave {
     return r.x + r.y;
   }
 
-  // Scores of BK keys in LDS.
+  // Operands from LDS: of product i of the scores (tile i % kTiles, elements 16 c ..,
+  // c = i / kTiles) and of the values (block i % kBlocks, keys 16 c .., c = i / kBlocks).
+  struct Operands {
+    const uint8_t *k, *v;
+    uint32_t kx, vx;
+
+    __device__ Operands(const uint8_t *keys, const uint8_t *values) {
+      const uint32_t lane = threadIdx.x & 63, half = lane >> 5;
+      k = keys + (lane & 31) * (D * 2);
+      kx = half ^ k_swizzle<D>(lane & 31);
+      const uint32_t row = 4 * half + (lane & 15) / 4, quad = lane & 3;
+      v = values + row * (D * 2) + (quad & 1) * 8;
+      vx = (2 * ((lane >> 4) & 1) + quad / 2) ^ v_swizzle<D>(row);
+    }
+    __device__ uint4 key(int i) const {
+      const int c = i / kTiles, t = i % kTiles;
+      return *reinterpret_cast<const uint4 *>(k + ((((2 * c) & 7) ^ kx) << 4) + t * (32 * D * 2) +
+                                              (((2 * c) & ~7) << 4));
+    }
+    __device__ uint4 value(int i) const {
+      const int c = i / kBlocks, b = i % kBlocks;
+      const uint8_t *const at = v + ((((4 * b) & 15) ^ vx) << 4) + (16 * c) * (D * 2) + (((4 * b) & ~15) << 4);
+      const uint2 x = read_tr(at), y = read_tr(at + 8 * (D * 2));
+      return make_uint4(x.x, x.y, y.x, y.y);
+    }
+  };
+  static constexpr int kScoreProducts = kSteps * kTiles, kValueProducts = 2 * kTiles * kBlocks;
+  static constexpr int kAhead = 3;  // products that operands are read ahead of theirs
+
+  // Scores of BK keys in LDS.  A single tile's long sums are taken in two halves: a
+  // product that waits for the one before takes twice as long (dim 256: 22.8 -> 20.4 us
+  // for the 816-row prefill; of 4 products the halves' sum costs what it saves).
   __device__ void scores(f32x16_t (&s)[kTiles], const uint8_t *k) const {
-    const uint32_t lane = threadIdx.x & 63, row = lane & 31, half = lane >> 5;
-    const uint8_t *const base = k + row * (D * 2);
-    const uint32_t x = half ^ k_swizzle<D>(row);
+    const Operands from(k, k);
+    constexpr int kSums = kTiles == 2 || kSteps >= 8 ? 2 : 1;
+    f32x16_t sum[kSums];
 #pragma unroll
-    for (int t = 0; t < kTiles; ++t) s[t] = f32x16_t(0.f);
+    for (int i = 0; i < kSums; ++i) sum[i] = f32x16_t(0.f);
+    uint4 f[kScoreProducts];
 #pragma unroll
-    for (int c = 0; c < kSteps; ++c)
+    for (int i = 0; i < kAhead; ++i) f[i] = from.key(i);
 #pragma unroll
-      for (int t = 0; t < kTiles; ++t) {
-        const uint4 a = *reinterpret_cast<const uint4 *>(base + t * (32 * D * 2) + (((2 * c) & ~7) << 4) +
-                                                         ((((2 * c) & 7) ^ x) << 4));
-        s[t] = mfma32<T>(a, q[c], s[t]);
-      }
+    for (int i = 0; i < kScoreProducts; ++i) {
+      __builtin_amdgcn_sched_barrier(0);
+      sum[i % kSums] = mfma32<T>(f[i], q[i / kTiles], sum[i % kSums]);
+      if (i + kAhead < kScoreProducts) f[i + kAhead] = from.key(i + kAhead);
+    }
+    s[0] = sum[0];
+    if (kTiles == 2)
+      s[kTiles - 1] = sum[kSums - 1];
+    else if (kSums == 2)
+      s[0] += sum[kSums - 1];
   }
 
-  // From scores to p, with the maximum and sum of each row; p in pairs.
-  __device__ void softmax(const AttnArgs &a, f32x16_t (&s)[kTiles], uint32_t (&p)[kTiles][8], int32_t k0,
-                          uint32_t missing) {
+  // Capped: in units of log2 e, as the exponent takes them.
+  __device__ static float capped(const AttnArgs &a, float s) {
+    const float e = __builtin_amdgcn_exp2f(s * a.scale2);
+    return __builtin_fmaf(-2.f * a.cap2, __builtin_amdgcn_rcpf(1.f + e), a.cap2);
+  }
+
+  // Scores of keys from k0 on that a row does not see become -infinity, and its
+  // maximum is raised where they call for it
+  // (top: the maximum of the scores as they are).
+  __device__ static float top_of(const f32x16_t (&s)[kTiles]) {
+    float top = s[0][0];
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) top = fmaxf(top, s[t][i]);
+    return top;
+  }
+  __device__ void settle(const AttnArgs &a, f32x16_t (&s)[kTiles], float top, int32_t k0, uint32_t missing) {
     const int half = (threadIdx.x & 63) >> 5;
     const float c = CAP ? 1.f : a.scale2;
-    if (CAP) {
-#pragma unroll
-      for (int t = 0; t < kTiles; ++t)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const float e = __builtin_amdgcn_exp2f(s[t][i] * a.scale2);
-          s[t][i] = __builtin_fmaf(-2.f * a.cap2, __builtin_amdgcn_rcpf(1.f + e), a.cap2);
-        }
-    }
     if (k0 < all_lo || k0 + BK > all_hi || missing) {
       masked = true;
 #pragma unroll
@@ -369,12 +422,8 @@ struct Wave {
           const bool see = key >= lo && key < hi && !(missing >> (2 * t + i / 8) & 1);
           s[t][i] = see ? s[t][i] : -INFINITY;
         }
+      top = top_of(s);
     }
-    float top = s[0][0];
-#pragma unroll
-    for (int t = 0; t < kTiles; ++t)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) top = fmaxf(top, s[t][i]);
     top = row_max(top);
     if (__ballot((top - m) * c > 8.f)) {
       const float to = fmaxf(m, top);
@@ -384,39 +433,100 @@ struct Wave {
 #pragma unroll
       for (int b = 0; b < kBlocks; ++b) o[b] *= f;  // whole vectors: by element, the loop would copy them
     }
-    const float base = m == -INFINITY ? 0.f : -m * c;
+  }
+
+  // What settled scores' exponents start from, and a pair's weights.
+  __device__ float base_of(const AttnArgs &a) const { return m == -INFINITY ? 0.f : CAP ? -m : -m * a.scale2; }
+  __device__ uint32_t pair(const AttnArgs &a, float base, float x, float y) {
+    const float c = CAP ? 1.f : a.scale2;
+    const float u = __builtin_amdgcn_exp2f(__builtin_fmaf(x, c, base));
+    const float v = __builtin_amdgcn_exp2f(__builtin_fmaf(y, c, base));
+    l += u + v;
+    return pack2<T>(u, v);
+  }
+
+  // From scores to p, with the maximum and sum of each row; p in pairs.
+  __device__ void softmax(const AttnArgs &a, f32x16_t (&s)[kTiles], uint32_t (&p)[kTiles][8], int32_t k0,
+                          uint32_t missing) {
+    if (CAP) {
+#pragma unroll
+      for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[t][i] = capped(a, s[t][i]);
+    }
+    settle(a, s, top_of(s), k0, missing);
+    const float base = base_of(a);
 #pragma unroll
     for (int t = 0; t < kTiles; ++t)
 #pragma unroll
-      for (int i = 0; i < 16; i += 2) {
-        const float u = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][i], c, base));
-        const float v = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][i + 1], c, base));
-        l += u + v;
-        p[t][i / 2] = pack2<T>(u, v);
+      for (int i = 0; i < 8; ++i) p[t][i] = pair(a, base, s[t][2 * i], s[t][2 * i + 1]);
+  }
+
+  // The scores of the next tile beside the weights of this one, then this one's
+  // values beside the cap and the maximum of the next one's scores: a lone wave's
+  // vector instructions issue while its matrix instructions, which do not wait for
+  // them, execute.  Left to itself the compiler issues the matrix instructions in
+  // runs, so the order is written out: operands are read kAhead products ahead, and
+  // nothing moves from one product's group to another's.  Returns the maximum.
+  __device__ float step(const AttnArgs &a, const f32x16_t (&s)[kTiles], f32x16_t (&next)[kTiles],
+                        const uint8_t *k, const uint8_t *v) {
+    constexpr int QK = kScoreProducts, PV = kValueProducts, kPairs = 8 * kTiles;
+    const Operands from(k, v);
+    uint4 f[QK + PV];
+    auto read = [&](int i) __attribute__((always_inline)) {
+      if (i < QK)
+        f[i] = from.key(i);
+      else if (i < QK + PV)
+        f[i] = from.value(i - QK);
+    };
+    uint32_t p[kPairs];
+    const float base = base_of(a);
+    float top = -INFINITY;
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t) next[t] = f32x16_t(0.f);
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) read(i);
+#pragma unroll
+    for (int i = 0; i < QK + PV; ++i) {
+      __builtin_amdgcn_sched_barrier(0);
+      if (i < QK) {
+        next[i % kTiles] = mfma32<T>(f[i], q[i / kTiles], next[i % kTiles]);
+      } else {
+        const int c = (i - QK) / kBlocks, b = (i - QK) % kBlocks;
+        o[b] = mfma32<T>(f[i], make_uint4(p[4 * c], p[4 * c + 1], p[4 * c + 2], p[4 * c + 3]), o[b]);
       }
+      read(i + kAhead);
+      // pairs of weights: spread over the products up to the middle of the values'
+#pragma unroll
+      for (int n = kPairs * i / (QK + PV / 2); n < kPairs * (i + 1) / (QK + PV / 2); ++n)
+        if (n < kPairs) p[n] = pair(a, base, s[n / 8][2 * (n % 8)], s[n / 8][2 * (n % 8) + 1]);
+      if (i >= QK) {
+#pragma unroll
+        for (int n = 16 * kTiles * (i - QK) / PV; n < 16 * kTiles * (i - QK + 1) / PV; ++n) {
+          if (CAP) next[n / 16][n % 16] = capped(a, next[n / 16][n % 16]);
+          top = fmaxf(top, next[n / 16][n % 16]);
+        }
+      }
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    return top;
   }
 
   // O^T += V^T P^T over BK keys in LDS.
   __device__ void values(const uint32_t (&p)[kTiles][8], const uint8_t *v) {
-    const uint32_t lane = threadIdx.x & 63, half = lane >> 5;
-    const uint32_t row = 4 * half + (lane & 15) / 4, quad = lane & 3;
-    const uint32_t x = (2 * ((lane >> 4) & 1) + quad / 2) ^ v_swizzle<D>(row);
-    const uint8_t *const base = v + row * (D * 2) + (quad & 1) * 8;
+    const Operands from(v, v);
+    uint4 f[kValueProducts];
 #pragma unroll
-    for (int c = 0; c < 2 * kTiles; ++c) {
+    for (int i = 0; i < kAhead; ++i) f[i] = from.value(i);
+#pragma unroll
+    for (int i = 0; i < kValueProducts; ++i) {
+      __builtin_amdgcn_sched_barrier(0);
+      const int c = i / kBlocks, b = i % kBlocks;
       const uint32_t *w = &p[c / 2][4 * (c % 2)];
-      const uint4 pb = make_uint4(w[0], w[1], w[2], w[3]);
-#pragma unroll
-      for (int b = 0; b < kBlocks; ++b) {
-        const uint8_t *const at = base + ((((4 * b) & 15) ^ x) << 4) + (16 * c) * (D * 2) + (((4 * b) & ~15) << 4);
-        auto read = [](const uint8_t *p) {
-          return __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                                               (__attribute__((address_space(3))) s16x4_t *)p));
-        };
-        const uint2 v0 = read(at), v1 = read(at + 8 * (D * 2));
-        o[b] = mfma32<T>(make_uint4(v0.x, v0.y, v1.x, v1.y), pb, o[b]);
-      }
+      o[b] = mfma32<T>(f[i], make_uint4(w[0], w[1], w[2], w[3]), o[b]);
+      if (i + kAhead < kValueProducts) f[i + kAhead] = from.value(i + kAhead);
     }
+    __builtin_amdgcn_sched_barrier(0);
   }
 
   __device__ bool finite() const {
@@ -642,45 +752,65 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) attn_tile_kernel(AttnAr
   Copy<D, true> vc;
   kc.begin();
   vc.begin();
-  // 16 keys and values to each wave, or (tiles of 32 keys) 16 keys or 16 values
-  auto request = [&](int32_t t) {
+  // Keys are copied two tiles ahead and values one: 16 keys and 16 values to each
+  // wave, or (tiles of 32 keys) 16 keys to the first two waves, 16 values to the others.
+  const int part = wv % (BK / 16);
+  Block there{0, 0};       // of the tile whose keys were requested last
+  uint32_t gone = 0, gone1 = 0;  // missing pages of that tile, and of the one before
+  auto keys = [&](int32_t t) {
     const int32_t k0 = t * BK;
-    const uint32_t to = base + (uint32_t)(t & 1) * (2 * kTile);
     pg.reach(k0 >> a.page_shift);
-    const int part = wv % (BK / 16);
-    const Block b = block_of<D>(a, pg, kh, k0 + 16 * part, it.kv);
-    const uint32_t at = to + part * (16 * D * 2);
-    if (BK == 64 || wv < 2) kc.issue(a.o.cache.k, b, at);
-    if (BK == 64 || wv >= 2) vc.issue(a.o.cache.v, b, at + kTile);
-    return missing_of<BK>(pg, k0, it.kv, a.page_shift);
+    there = block_of<D>(a, pg, kh, k0 + 16 * part, it.kv);
+    if (BK == 64 || wv < 2) kc.issue(a.o.cache.k, there, base + (t & 1) * kTile + part * (16 * D * 2));
+    gone1 = gone;
+    gone = missing_of<BK>(pg, k0, it.kv, a.page_shift);
   };
-  uint32_t gone = 0;
+  auto values = [&](int32_t t) {
+    if (BK == 64 || wv >= 2) vc.issue(a.o.cache.v, there, base + (2 + (t & 1)) * kTile + part * (16 * D * 2));
+  };
   if (t0 < t1) {
     pg.begin((t0 * BK) >> a.page_shift);
-    gone = request(t0);
-  }
-  auto next = [&](int32_t t) {
-    // tile t is in LDS, and every wave has done with the tile before it
+    keys(t0);
     wait_vm_barrier<0>();
-    const uint32_t missing = gone;
-    if (t + 1 < t1) gone = request(t + 1);
-    return missing;
+    values(t0);
+    if (t0 + 1 < t1) keys(t0 + 1);
+  }
+  // The keys of tile t + 1 and the values of tile t are in LDS, and every wave has
+  // done with the keys of t and the values of t - 1, whose room is filled next.
+  auto arrive = [&](int32_t t) {
+    wait_vm_barrier<0>();
+    if (t + 1 < t1) values(t + 1);
+    if (t + 2 < t1) keys(t + 2);
   };
-  // this wave's tiles, between those that only others need (three loops: sums that a
-  // branch in the loop may or may not change are copied, 64 registers a tile)
+  // This wave's tiles, c0 .. c1 - 1, between those that only others need (sums that a
+  // branch in the loop may or may not change would be copied, 64 registers a tile).
+  // Each step takes the scores of the tile after its own; the last one's are not used.
   const int32_t c0 = min(max(w.any_lo / BK, t0), t1), c1 = max(min((w.any_hi + BK - 1) / BK, t1), c0);
   int32_t t = t0;
-  for (; t < c0; ++t) next(t);
-  for (; t < c1; ++t) {
-    const uint32_t missing = next(t);
-    const uint8_t *k = lds + (t & 1) * (2 * kTile);
-    f32x16_t s[BK / 32];
-    uint32_t p[BK / 32][8];
-    w.scores(s, k);
-    w.softmax(a, s, p, t * BK, missing);
-    w.values(p, k + kTile);
+  f32x16_t s0[BK / 32], s1[BK / 32];
+  auto first = [&](int32_t at) {
+    w.scores(s0, lds + (at & 1) * kTile);
+    if (CAP) {
+#pragma unroll
+      for (int u = 0; u < BK / 32; ++u)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s0[u][i] = w.capped(a, s0[u][i]);
+    }
+    w.settle(a, s0, w.top_of(s0), at * BK, at + 1 < t1 ? gone1 : gone);
+  };
+  auto step = [&](const f32x16_t (&s)[BK / 32], f32x16_t (&n)[BK / 32]) {
+    arrive(t);
+    const float top = w.step(a, s, n, lds + ((t + 1) & 1) * kTile, lds + (2 + (t & 1)) * kTile);
+    if (t + 1 < c1) w.settle(a, n, top, (t + 1) * BK, t + 2 < t1 ? gone1 : gone);
+    return ++t < c1;
+  };
+  if (c0 < c1) {
+    for (; t < c0; ++t) arrive(t);
+    first(c0);
+    while (step(s0, s1) && step(s1, s0)) {
+    }
   }
-  for (; t < t1; ++t) next(t);
+  for (; t < t1; ++t) arrive(t);
 
   w.l = Wave<T, D, BK, CAP>::row_sum(w.l);
   const bool split = it.splits > 1;
@@ -902,10 +1032,10 @@ __global__ void __launch_bounds__(256, kStreamWgs<D>) attn_stream_kernel(AttnArg
 }
 
 // Joins the splits of a tile's rows, in an order that the number of splits decides.
-// Up to 16: D / 4 lanes take a row.  More: a workgroup takes 64 elements of a row, 16
-// lanes reading a split's and 16 groups of lanes every 16th split, whose sums meet in
-// LDS; that many requests at once, since what other XCDs wrote comes from behind
-// this one's L2.
+// Up to 64: D / 4 lanes take a row, 8 splits at a time.  More: a workgroup takes 64
+// elements of a row, 16 lanes reading a split's and 16 groups of lanes every 16th
+// split, whose sums meet in LDS.  Either way as many requests at once as registers
+// hold, since what other XCDs wrote comes from behind this one's L2.
 template <int T, int D>
 __global__ void __launch_bounds__(256) attn_join_kernel(AttnArgs a) {
   constexpr int kLanes = D / 4, kPlaces = 256 / kLanes, kParts = D / 64;
@@ -931,29 +1061,33 @@ __global__ void __launch_bounds__(256) attn_join_kernel(AttnArgs a) {
     v.z = __builtin_fmaf(x.z, f, v.z);
     v.w = __builtin_fmaf(x.w, f, v.w);
   };
-  if (it.splits <= 16) {
+  if (it.splits <= 64) {
     const int place = threadIdx.x / kLanes, d0 = 4 * (threadIdx.x % kLanes);
     for (int32_t r = blockIdx.y * kPlaces + place; r < it.rows; r += gridDim.y * kPlaces) {
-      // all requests at once, those past the last split repeating it and left out
-      float2 ml[16];
       float m = -INFINITY, l = 0.f;
-#pragma unroll
-      for (int i = 0; i < 16; ++i) ml[i] = *part_ml(a, base + min(i, it.splits - 1), r, D);
       float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-      for (int i = 0; i < 16; ++i) m = fmaxf(m, ml[i].x);
-#pragma unroll
-      for (int s0 = 0; s0 < 16; s0 += 8) {
-        if (s0 >= it.splits) break;
+      for (int32_t s0 = 0; s0 < it.splits; s0 += 8) {
+        // (those past the last split repeat it and are left out)
+        float2 ml[8];
         float4 x[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-          x[i] = *reinterpret_cast<const float4 *>(part_o(a, base + min(s0 + i, it.splits - 1), r, D) + d0);
+        for (int i = 0; i < 8; ++i) {
+          const int64_t item = base + min(s0 + i, it.splits - 1);
+          ml[i] = *part_ml(a, item, r, D);
+          x[i] = *reinterpret_cast<const float4 *>(part_o(a, item, r, D) + d0);
+        }
+        float to = m;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) to = fmaxf(to, ml[i].x);
+        const float f0 = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - to);
+        m = to;
+        l *= f0;
+        v = make_float4(v.x * f0, v.y * f0, v.z * f0, v.w * f0);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           if (s0 + i >= it.splits) continue;
-          const float f = ml[s0 + i].x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml[s0 + i].x - m);
-          l = __builtin_fmaf(ml[s0 + i].y, f, l);
+          const float f = ml[i].x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml[i].x - m);
+          l = __builtin_fmaf(ml[i].y, f, l);
           add(v, x[i], f);
         }
       }
@@ -1027,7 +1161,7 @@ hipError_t attn_launch_d(const AttnArgs &a, hipStream_t s) {
   // one workgroup for each 1024 / D rows, or, of few tiles, up to one for each 64
   // elements of a row
   const uint32_t tiles = a.tiles * (uint32_t)a.o.cache.heads, rows = (uint32_t)a.part_rows;
-  const uint32_t least = (rows * D + 1023) / 1024, most = 512 / tiles, parts = rows * (D / 64);
+  const uint32_t least = (rows * D + 1023) / 1024, most = 2048 / tiles, parts = rows * (D / 64);
   const uint32_t spare = parts < most ? parts : most;
   attn_join_kernel<T, D><<<dim3(tiles, least > spare ? least : spare), 256, 0, s>>>(a);
   return hipGetLastError();
