@@ -11,6 +11,7 @@ namespace eb {
 
 constexpr int kMaxBatch = 4096;
 constexpr int kMaxSplits = 1024;  // of a row tile
+constexpr int kScanBatch = 64;    // sequences that every wave looks over itself
 
 hipError_t launch_kv_extend(const eb_kv_extend_op &o, hipStream_t s);
 hipError_t launch_rope_append(const eb_rope_append_op &o, hipStream_t s);
@@ -21,6 +22,8 @@ hipError_t launch_attention(const eb_attention_op &o, void *ws, hipStream_t s);
 struct AttnArgs {
   eb_attention_op o;
   float *ws;           // sums of splits
+  int4 *item_table;    // batch > kScanBatch: items' (sequence or -1, tile, split, splits)
+  int4 *tile_table;    // and tiles' (sequence or -1, tile, first item, splits)
   int64_t head_rows;   // cache rows of a page: heads * page
   int32_t page_shift;
   int32_t kv_max;      // keys of a table row

@@ -648,9 +648,10 @@ def rope_append(qkv: torch.Tensor, cache: KVCache, slots: torch.Tensor, position
     each rotated pair, 2 * len(freqs) elements of a head being rotated."""
     dev, dim = cache.index, cache.dim
     width = (q_heads + 2 * cache.heads) * dim
-    _need(qkv.dim() == 2 and qkv.shape[1] == width and qkv.get_device() == dev and qkv.dtype in DTYPES
-          and qkv.stride(1) == 1,
-          f"qkv: rows of {width} float32, float16 or bfloat16 values on cuda:{dev}")
+    qkv_type = DTYPES.get(qkv.dtype)
+    if qkv.dim() != 2 or qkv_type is None or qkv.get_device() != dev or qkv.stride(1) != 1 \
+            or qkv.shape[1] != width:
+        raise ValueError(f"qkv: rows of {width} float32, float16 or bfloat16 values on cuda:{dev}")
     rows = qkv.shape[0]
     if out is None:
         out = torch.empty((rows, q_heads, dim), dtype=cache.dtype, device=cache.device)
@@ -667,7 +668,7 @@ def rope_append(qkv: torch.Tensor, cache: KVCache, slots: torch.Tensor, position
         cache.k.data_ptr(), cache.v.data_ptr(), *cache.shape, qkv.data_ptr(), out.data_ptr(),
         _ints("slots", slots, dev, rows), pos, _floats("freqs", freqs, dev, half),
         _floats("q_norm", q_norm, dev, dim), _floats("k_norm", k_norm, dev, dim),
-        qkv.stride(0) if rows > 1 else width, q_stride, pos_stride, DTYPES[qkv.dtype], q_heads, rows,
+        qkv.stride(0) if rows > 1 else width, q_stride, pos_stride, qkv_type, q_heads, rows,
         2 * half, STYLES[style], axes, *(sections + (0, 0))[:3], eps)
     _check(_launch(_rope_append, op, dev), "eb_rope_append")
     return out
@@ -701,7 +702,7 @@ def attention(q: torch.Tensor, cache: KVCache, table: torch.Tensor, q_start: tor
         dim ** -0.5 if scale is None else scale, softcap)
     if workspace is not None:
         _need(workspace.dtype is torch.uint8 and workspace.get_device() == dev and workspace.is_contiguous(),
-              f"workspace: contiguous uint8 on cuda:{dev}")
+              "workspace: contiguous uint8 on the cache's GPU")
         _check(_launch(_attention, op, dev, workspace.data_ptr(), workspace.numel()), "eb_attention")
         return out
     # its size, by what it depends on, is kept after a call that succeeded
