@@ -553,6 +553,8 @@ def _heads(name: str, t: torch.Tensor, dev: int, dtype, rows: int, heads: int, d
     """Stride between the rows of t [rows, heads, dim], whose rows are contiguous."""
     if t.dtype is not dtype or t.get_device() != dev or t.shape != (rows, heads, dim):
         raise ValueError(f"{name}: {dtype} values of shape {(rows, heads, dim)} on cuda:{dev}")
+    if t.is_contiguous():
+        return heads * dim
     stride, head, elem = t.stride()
     if elem != 1 or (head != dim and heads != 1):
         raise ValueError(f"{name}: rows of contiguous heads")
@@ -560,6 +562,7 @@ def _heads(name: str, t: torch.Tensor, dev: int, dtype, rows: int, heads: int, d
 
 
 _get_device = torch._C._cuda_getDevice
+_capturing = torch._C._cuda_isCurrentStreamCapturing
 
 
 def _launch(fn, op: bytes, dev: int, *more) -> int:
@@ -685,13 +688,14 @@ def attention(q: torch.Tensor, cache: KVCache, table: torch.Tensor, q_start: tor
     one the call takes one from scratch(), or, under graph capture, a fresh one
     that belongs to the graph."""
     dev, dim = cache.index, cache.dim
-    _need(q.dim() == 3 and table.dim() == 2, "q: [rows, q_heads, dim]; table: [batch, stride]")
+    if q.dim() != 3 or table.dim() != 2:
+        raise ValueError("q: [rows, q_heads, dim]; table: [batch, stride]")
     rows, q_heads, _ = q.shape
     batch, stride = table.shape
     q_stride = _heads("q", q, dev, cache.dtype, rows, q_heads, dim)
     if out is None:
-        out = torch.empty((rows, q_heads, dim), dtype=cache.dtype, device=cache.device)
         out_stride = q_heads * dim
+        out = torch.empty_like(q) if q_stride == out_stride else q.new_empty((rows, q_heads, dim))
     else:
         out_stride = _heads("out", out, dev, cache.dtype, rows, q_heads, dim)
     op = _PACK_ATTN.pack(
@@ -714,7 +718,7 @@ def attention(q: torch.Tensor, cache: KVCache, table: torch.Tensor, q_start: tor
     if not nbytes:
         st = _launch(_attention, op, dev, None, 0)
     else:
-        if torch.cuda.is_current_stream_capturing():
+        if _capturing():
             ws = torch.empty(nbytes, dtype=torch.uint8, device=cache.device)
         else:
             ws = _SCRATCH.get((dev, _raw_stream(dev)))

@@ -117,6 +117,24 @@ def test_attention_refusals(eb, kw, status):
     assert _attn(eb, **kw) == status
 
 
+def test_attention_workspace(eb):
+    """Needed where keys are split over workgroups or the batch is large; refused if too small."""
+    size = eb.lib.eb_attention_workspace_bytes
+
+    def need(**kw):
+        return size(ctypes.byref(_attn_op(eb, **kw)))
+    assert need(batch=1, rows=1, max_new=1, max_kv=64) == 0          # one unit of keys: one workgroup a head
+    split = need(batch=1, rows=1, max_new=1, max_kv=4000)
+    assert split > 0 and split % 256 == 0
+    assert need(batch=1, rows=4096, max_new=4096, max_kv=4096, q_heads=32, q_stride=4096, out_stride=4096,
+                cache_heads=32) == 0                                 # tiles enough for the GPU
+    assert need(batch=65, rows=65, max_new=1, max_kv=64) > 0         # its items' tables
+    assert need(batch=64, rows=64, max_new=1, max_kv=64) == 0
+    op = dict(batch=1, rows=1, max_new=1, max_kv=4000)
+    assert _attn(eb, ws=20 * GB, wsb=split - 256, **op) == -1
+    assert _attn(eb, ws=None, wsb=0, **op) == -1
+
+
 def test_no_rows_is_a_no_op(eb):
     assert _rope(eb, rows=0, qkv=0, q_out=0, slots=0, positions=0, freqs=0) == 0
     assert _attn(eb, ws=None, wsb=0, rows=0, q=0, out=0, table=0, q_start=0, kv_len=0) == 0

@@ -235,6 +235,35 @@ def test_attn_masks(eb, mask, prefix, window, cap, d):
           prefix=prefix, window=window, cap=cap, seed=window + 3)
 
 
+# 64 query heads for each of 4: sequences whose 128-row tiles fill the GPU, which
+# take the kernel that shares key tiles between four waves of rows
+WIDE = dict(hq=256, hkv=4)
+
+
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("dtype", [BF, FP])
+@pytest.mark.parametrize("mask,prefix,window,cap,kv", [
+    ("causal", None, 0, 0.0, 130), ("causal", None, 0, 0.0, 423), ("full", None, 0, 0.0, 161),
+    ("causal", [90], 0, 20.0, 200), ("causal", None, 21, 0.0, 300), ("full", None, 40, 5.0, 257)])
+def test_attn_row_tiles(eb, d, dtype, mask, prefix, window, cap, kv):
+    _attn(eb, [(130, kv)], d=d, dtype=dtype, mask=mask, prefix=prefix, window=window, cap=cap, seed=kv, **WIDE)
+
+
+@pytest.mark.parametrize("d,page", [(64, 16), (128, 32), (128, 128), (256, 16), (256, 64)])
+def test_attn_row_tiles_ragged(eb, d, page):
+    """Tiles of many sequences, one of them long enough to be split; tokens past max_new,
+    rows that see nothing, padding."""
+    seqs = [(100, 100), (1, 40), (31, 500), (0, 7), (3, 2), (40, 3000), (2, 0), (15, 16)]
+    _attn(eb, seqs, d=d, dtype=BF, page=page, seed=d + page, pad=4, **WIDE)
+    _attn(eb, seqs, d=d, dtype=BF, page=page, seed=d + page, mask="full", max_new=37, hq=384, hkv=6)
+
+
+def test_attn_row_tiles_many_sequences(eb):
+    rng = np.random.default_rng(3)
+    seqs = [(int(rng.integers(0, 6)), int(rng.integers(1, 60))) for _ in range(90)] + [(20, 2500), (7, 7)]
+    _attn(eb, seqs, d=64, dtype=FP, seed=4, pad=2, **WIDE)
+
+
 def test_attn_sharp_scores(eb):
     """Scores far apart, of both signs, a scale of one, a negative one and none."""
     for i, (gain, scale) in enumerate(((30.0, None), (4.0, 1.0), (2.0, -0.3), (1.0, 0.0))):
@@ -266,13 +295,13 @@ def test_attn_empty_rows_and_padding(eb):
 
 
 @pytest.mark.parametrize("bad", [float("nan"), float("inf"), float("-inf"), 3e38])
-@pytest.mark.parametrize("d", [64, 128, 256])
-def test_attn_masked_places_hold_anything(eb, bad, d):
+@pytest.mark.parametrize("d,hq,hkv", [(64, 4, 2), (128, 4, 2), (256, 4, 2), (64, 256, 4), (128, 256, 4), (256, 256, 4)])
+def test_attn_masked_places_hold_anything(eb, bad, d, hq, hkv):
     """Cache rows past a sequence's end, pages of nobody, keys and values that the causal
     mask, the window or the missing page hides."""
     new, lens, page = [37, 1, 100], [90, 33, 100], 16
-    k, v, table = A.paged(lens, page, 2, d, BF, seed=5)
-    q = (_randn(138, 4, d, seed=6) * 1.5).to(BF)
+    k, v, table = A.paged(lens, page, hkv, d, BF, seed=5)
+    q = (_randn(138, hq, d, seed=6) * 1.5).to(BF)
     used = torch.zeros(k.shape[0] * page, dtype=torch.bool)
     for b, t in enumerate(lens):
         j = torch.arange(t)
@@ -280,7 +309,7 @@ def test_attn_masked_places_hold_anything(eb, bad, d):
 
     def spoil(c, cells):
         c = c.transpose(1, 2).contiguous()
-        c.view(-1, 2, d)[cells.to(DEV)] = bad
+        c.view(-1, hkv, d)[cells.to(DEV)] = bad
         return c.transpose(1, 2).contiguous()
 
     args = (table, A.starts(new), A.ints(lens), 100, 100)
@@ -317,12 +346,22 @@ def test_attn_wild_lengths_stay_in_bounds(eb):
     """Offsets and lengths that are no such thing are clamped to their arrays."""
     k, v, table = A.paged([64, 64], 16, 2, 64, BF, seed=3)
     cache = eb.KVCache(k, v)
-    q = _randn(20, 4, 64, seed=4, dtype=BF)
-    for q_start in ([0, 10, 2 ** 31 - 1], [-5, 10, 20], [15, 3, 20], [0, 2 ** 31 - 1, -2 ** 31], [20, 25, 30]):
-        for kv in ([2 ** 31 - 1, 64], [-3, -2 ** 31]):
-            out = torch.full_like(q, 7.0)
-            eb.attention(q, cache, table, A.ints(q_start), A.ints(kv), 20, 64, out=out)
-            assert bool(torch.isfinite(out).all())
+    for hq in (4, 1024):   # few rows, and 128-row tiles
+        q = _randn(20, hq, 64, seed=4, dtype=BF)
+        for q_start in ([0, 10, 2 ** 31 - 1], [-5, 10, 20], [15, 3, 20], [0, 2 ** 31 - 1, -2 ** 31], [20, 25, 30]):
+            for kv in ([2 ** 31 - 1, 64], [-3, -2 ** 31]):
+                for pre in (None, [2 ** 31 - 1, -2 ** 31]):
+                    out = torch.full_like(q, 7.0)
+                    eb.attention(q, cache, table, A.ints(q_start), A.ints(kv), 20, 64, out=out,
+                                 prefix=None if pre is None else A.ints(pre))
+                    assert bool(torch.isfinite(out).all())
+    # many sequences that all claim all rows: more tiles than there can be
+    q = _randn(200, 32, 64, seed=4, dtype=BF)
+    batch = 600
+    many = table[:1].repeat(batch, 1)
+    out = torch.full_like(q, 7.0)
+    eb.attention(q, cache, many, A.ints([0, 200] * (batch // 2) + [0]), A.ints([64] * batch), 200, 64, out=out)
+    assert bool(torch.isfinite(out).all())
 
 
 def test_attn_strided_rows_and_scratch(eb):
@@ -504,6 +543,29 @@ def test_step_captured_and_replayed(eb):
     torch.cuda.synchronize()
     for _, _, y in graphs:
         assert torch.equal(y, want)
+
+
+def test_large_batch_captured(eb):
+    """A batch whose items a kernel lays out first, captured and replayed as lengths change."""
+    batch = 130
+    lens = [int(t) for t in np.random.default_rng(5).integers(1, 300, batch)]
+    k, v, table = A.paged(lens, 16, 1, 64, BF, seed=6)
+    cache = eb.KVCache(k, v)
+    q = _randn(batch, 8, 64, seed=7, dtype=BF)
+    q_start, kv_len = A.starts([1] * batch), A.ints(lens)
+    args = (cache, table, q_start, kv_len, 1, 300)
+    eb.attention(q, *args)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        out = eb.attention(q, *args)
+    for it in range(4):
+        want = eb.attention(q, *args).clone()
+        out.zero_()
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want), it
+        kv_len.copy_((kv_len * 3 // 4).clamp(min=1))
 
 
 def test_other_stream(eb):
