@@ -157,7 +157,8 @@ eb_status eb_rope_append(const eb_rope_append_op *op, hipStream_t stream);
  * kv_len: they decide the launch; tokens past max_new are not computed (their
  * rows stay), keys past max_kv are still seen.
  * Products take the 16-bit values on the matrix cores with fp32 sums; running
- * maxima and sums of the softmax are fp32.  The weights e^{t - max} are rounded
+ * maxima and sums of the softmax are fp32; capped scores are off by at most
+ * softcap * 2^-20, which is why caps past 2^10 are not taken.  The weights e^{t - max} are rounded
  * once to the cache's type for the second product (each off by at most 2^-8 of
  * itself for EB_BF16, 2^-11 for EB_F16), as is the output.
  * With several sequences, or few rows, the keys of a row are split over
@@ -181,8 +182,8 @@ typedef struct {
   int32_t max_kv;         /* >= 1 */
   int32_t mask;           /* EB_MASK_CAUSAL or EB_MASK_FULL */
   int32_t window;         /* >= 0; 0: none */
-  float scale;            /* finite */
-  float softcap;          /* finite, >= 0; 0: none */
+  float scale;            /* |scale| <= 65536 */
+  float softcap;          /* 0: none, or 2^-10 .. 2^10 */
 } eb_attention_op;
 
 /* Bytes of workspace eb_attention needs for *op: the fp32 sums of rows whose

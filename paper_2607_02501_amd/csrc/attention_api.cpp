@@ -134,7 +134,8 @@ eb_status check_attention(const eb_attention_op &o) {
       (int64_t)o.table_stride * o.cache.page > kMaxKeys || o.max_new < 1 || o.max_kv < 1 || o.window < 0 ||
       (o.mask != EB_MASK_CAUSAL && o.mask != EB_MASK_FULL))
     return EB_ERR_INVALID;
-  if (!std::isfinite(o.scale) || !(std::isfinite(o.softcap) && o.softcap >= 0.0f)) return EB_ERR_INVALID;
+  if (!(std::fabs(o.scale) <= 65536.0f) || !(std::isfinite(o.softcap) && o.softcap >= 0.0f)) return EB_ERR_INVALID;
+  if (o.softcap > 0.0f && (o.softcap < 0x1p-10f || o.softcap > 0x1p10f)) return EB_ERR_UNSUPPORTED;
   if (o.rows == 0) return EB_OK;
   if (!o.q || !o.out || !o.table || !o.q_start || !o.kv_len) return EB_ERR_INVALID;
   if (o.q_stride % 8 != 0 || o.out_stride % 8 != 0 || !aligned(o.q, 16) || !aligned(o.out, 16) ||

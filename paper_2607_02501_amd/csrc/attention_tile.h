@@ -580,7 +580,7 @@ __device__ inline uint32_t missing_of(const Pages &pg, int32_t k0, int32_t kv, i
 }
 
 // Many rows: 128 of a tile, 32 to each wave, all waves over the same keys, which
-// are copied to LDS one tile ahead (one barrier a tile).
+// are copied to LDS ahead of their use (one barrier a tile).
 template <int T, int D, int BK, bool CAP>
 __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) attn_tile_kernel(AttnArgs a) {
   constexpr int kTile = BK * D * 2;  // bytes of a tile of keys or values
@@ -715,6 +715,7 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) attn_tile_kernel(AttnAr
   // rows whose sums took up an infinity or NaN where some key was hidden
   uint64_t again = __ballot(live && w.masked && !w.finite());
   again = (again | again >> 32) & 0xffffffffu;
+  if (again) wait_vm<0>();  // what is written again has been written
   while (again) {
     const int src = __builtin_ctzll(again);
     again &= again - 1;
@@ -879,6 +880,10 @@ __global__ void __launch_bounds__(256, kStreamWgs<D>) attn_stream_kernel(AttnArg
   }
   __syncthreads();
   uint32_t todo = again;
+  if (todo) {  // what is written again has been written
+    wait_vm<0>();
+    __syncthreads();
+  }
   for (; todo; todo &= todo - 1) {
     const int src = __builtin_ctz(todo);
     if (src % 4 != wv) continue;

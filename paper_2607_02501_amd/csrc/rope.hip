@@ -136,7 +136,8 @@ __global__ void __launch_bounds__(kThreads)
 #pragma unroll
       for (int d = kLanes / 2; d >= 1; d >>= 1) ss += __shfl_xor(ss, d);
       // 1 / sqrt to one step of fp32; its argument kept out of the subnormals
-      const float r = __builtin_amdgcn_rsqf(fmaxf(__builtin_fmaf(ss, 1.0f / D, o.norm_eps), 1.17549435e-38f));
+      const float ms = __builtin_fmaf(ss, 1.0f / D, o.norm_eps);
+      const float r = __builtin_amdgcn_rsqf(ms < 1.17549435e-38f ? 1.17549435e-38f : ms);
 #pragma unroll
       for (int j = 0; j < 8; ++j) x[j] = x[j] * r * (is_q ? gq[j] : gk[j]);
     }

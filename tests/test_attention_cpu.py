@@ -108,7 +108,8 @@ def test_rope_refusals(eb, kw, status):
     (dict(out_stride=1026), -2), (dict(table_stride=0), -1), (dict(table_stride=1 << 27), -1),
     (dict(rows=1 << 24, q_heads=256, q_stride=1 << 15, out_stride=1 << 15), -1), (dict(max_new=0), -1),
     (dict(max_kv=0), -1), (dict(window=-1), -1), (dict(mask=2), -1),
-    (dict(scale=float("inf")), -1), (dict(softcap=-1.0), -1), (dict(softcap=float("nan")), -1), (dict(q=0), -1),
+    (dict(scale=float("inf")), -1), (dict(scale=-65537.0), -1), (dict(scale=float("nan")), -1),
+    (dict(softcap=1025.0), -3), (dict(softcap=0.0009), -3), (dict(softcap=-1.0), -1), (dict(softcap=float("nan")), -1), (dict(q=0), -1),
     (dict(out=0), -1), (dict(table=0), -1), (dict(q_start=0), -1), (dict(kv_len=0), -1),
     (dict(q=3 * GB + 2), -2), (dict(out=4 * GB + 8), -2), (dict(prefix=8 * GB + 1), -2), (dict(out=3 * GB), -1),
     (dict(out=1 * GB + 256), -1), (dict(out=5 * GB), -1), (dict(ws=20 * GB + 64), -2), (dict(ws=0, wsb=16), -1),

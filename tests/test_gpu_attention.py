@@ -228,7 +228,8 @@ def test_attn_pages(eb, page):
 @pytest.mark.parametrize("mask,prefix,window,cap", [
     ("causal", [0, 20, 500, 3], 0, 0.0), ("causal", None, 1, 0.0), ("causal", None, 17, 0.0),
     ("causal", [40, 1, 64, 9], 33, 0.0), ("causal", None, 0, 5.0), ("full", None, 0, 30.0),
-    ("full", None, 25, 0.0), ("causal", [50, 50, 50, 50], 64, 10.0)])
+    ("full", None, 25, 0.0), ("causal", [50, 50, 50, 50], 64, 10.0), ("causal", None, 0, 2.0 ** -10),
+    ("causal", None, 50, 1024.0)])
 @pytest.mark.parametrize("d", [64, 128, 256])
 def test_attn_masks(eb, mask, prefix, window, cap, d):
     _attn(eb, [(40, 130), (64, 64), (1, 200), (100, 300)], 4, 1, d, BF if d != 64 else FP, mask=mask,
