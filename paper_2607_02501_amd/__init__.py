@@ -1,5 +1,5 @@
-"""MI355X-native block-quantized linear layers (Q8_0 / Q4_0) for batch-1
-embodied-model inference.
+"""MI355X-native block-quantized linear layers (Q8_0 / Q4_0 / Q6_S) for batch-1
+embodied-model inference, and the attention between them over a paged cache.
 
 Submodules:
   eb        -- Python binding of the C-ABI library libeb.so (HIP kernels for gfx950)

@@ -18,6 +18,11 @@ _FILES = {
     "q6": ("mfma_q6.hip", "mfma_common.h", "norm.hip") + _COMMON,
     "gemv_q6": ("gemv_q6.hip", "gemv_common.h") + _COMMON,
     "i8": ("mfma_i8.hip", "mfma_common.h") + _COMMON,
+    # attention over the paged cache, head rotation, the cache's bookkeeping
+    "attn": ("attention_tile.h", "attention_items.h", "attention.hip", "attention_bf16.hip",
+             "attention_f16.hip", "attention.h", "attention_api.cpp", "mfma_common.h", "epilogue.h"),
+    "rope": ("rope.hip", "attention.h", "attention_api.cpp", "epilogue.h"),
+    "kv": ("kv_extend.hip", "attention.h", "attention_api.cpp"),
 }
 
 
@@ -29,6 +34,12 @@ def family(symbol: str) -> str:
         return "gemv"
     if symbol.startswith("mm_i8") or symbol.startswith("quantize_x8"):
         return "i8"
+    if symbol.startswith("attn_"):
+        return "attn"
+    if symbol.startswith("rope_append"):
+        return "rope"
+    if symbol.startswith("kv_extend"):
+        return "kv"
     if symbol.startswith("mm_q6"):
         return "q6"
     if symbol.startswith("mm_"):
