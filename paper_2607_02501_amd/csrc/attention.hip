@@ -13,29 +13,39 @@ constexpr float kLog2e = 1.4426950408889634f;
 
 // The tables of a batch of more than kScanBatch sequences.  As in eb_kv_extend, each
 // workgroup sums over the whole batch itself and then fills its part: a wave of the
-// attention kernels would take 0.4 us for every 64 sequences (4000 of them: 25 us each).
+// attention kernels would take 0.4 us for every 64 sequences (single tokens of 1000
+// sequences: 127 us, 206 if every wave looks them over; of 4000, 352 and 1590).  Up to
+// kScanBatch = 64 a wave looks them over in one step, which is less than another launch
+// (500 keys each, 2 sequences: 11.0 us, with tables 13.2; 64 sequences: 28.7, 32.5).
 constexpr int kItemThreads = 512;
 __global__ void __launch_bounds__(kItemThreads) attn_items_kernel(AttnArgs a) {
   __shared__ uint32_t items[kMaxBatch + 1], tiles[kMaxBatch + 1];
   __shared__ uint32_t red[2][kItemThreads / 64];
   __shared__ float unit_red[kItemThreads / 64];
+  __shared__ int32_t long_red[kItemThreads / 64];
   const int32_t batch = a.o.batch, lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
   uint32_t per = 1;
   if (a.target > 0) {
     float units = 0.f;
+    int32_t longest = 0;
     for (int32_t b = threadIdx.x; b < batch; b += kItemThreads) {
       const Seq s = seq_of(a, b);
       units += (float)s.tiles * (float)s.units;
+      longest = max(longest, s.tiles > 0 ? s.units : 0);
     }
 #pragma unroll
-    for (int d = 32; d >= 1; d >>= 1) units += __shfl_xor(units, d);
-    if (lane == 0) unit_red[wv] = units;
+    for (int d = 32; d >= 1; d >>= 1) {
+      units += __shfl_xor(units, d);
+      longest = max(longest, __shfl_xor(longest, d));
+    }
+    if (lane == 0) unit_red[wv] = units, long_red[wv] = longest;
     __syncthreads();
     units = 0.f;
-    for (int w = 0; w < kItemThreads / 64; ++w) units += unit_red[w];
-    per = units_per_split(a, units);
+    for (int w = 0; w < kItemThreads / 64; ++w) units += unit_red[w], longest = max(longest, long_red[w]);
+    per = units_per_split(a, units, longest);
   }
   // (sums stop at 2^30: offsets that overlap without end may ask for more)
+  auto splits_of = [&](const Seq &s) { return a.target > 0 && s.units > 0 ? (s.units + per - 1) / per : 1u; };
   auto most = [](uint32_t x, uint32_t y) { return min(x + y, 1u << 30); };
   uint32_t item0 = 0, tile0 = 0;
   for (int32_t b0 = 0; b0 < batch; b0 += kItemThreads) {
@@ -43,8 +53,9 @@ __global__ void __launch_bounds__(kItemThreads) attn_items_kernel(AttnArgs a) {
     uint32_t n = 0, t = 0;
     if (b < batch) {
       const Seq s = seq_of(a, b);
-      t = s.tiles;
-      n = min(t * (a.target > 0 && s.units > 0 ? (s.units + per - 1) / per : 1), 1u << 30);
+      const uint32_t splits = splits_of(s);
+      n = min(s.tiles * splits, 1u << 30);
+      t = splits > 1 ? s.tiles : 0;
     }
     uint32_t sn = n, st = t;
 #pragma unroll
@@ -80,23 +91,32 @@ __global__ void __launch_bounds__(kItemThreads) attn_items_kernel(AttnArgs a) {
     int4 e = make_int4(-1, 0, 0, 1);
     if (at < item0) {
       const int32_t b = find(items, at);
-      const uint32_t t = tiles[b + 1] - tiles[b], splits = (items[b + 1] - items[b]) / max(t, 1u);
-      const uint32_t r = at - items[b];
-      e = make_int4(b, r / max(splits, 1u), r % max(splits, 1u), splits);
+      const Seq s = seq_of(a, b);
+      const uint32_t r = at - items[b], n = max(s.tiles, 1);
+      e = make_int4(b, r % n, r / n, splits_of(s));
     }
     a.item_table[at] = e;
   }
-  for (uint32_t at = at0; at < a.tiles; at += step) {
+  for (uint32_t at = at0; at < (uint32_t)a.join_tiles; at += step) {
     int4 e = make_int4(-1, 0, 0, 1);
     if (at < tile0) {
       const int32_t b = find(tiles, at);
-      const uint32_t t = tiles[b + 1] - tiles[b], splits = (items[b + 1] - items[b]) / max(t, 1u);
-      const uint32_t r = at - tiles[b];
-      e = make_int4(b, r, items[b] + r * splits, splits);
+      e = make_int4(b, at - tiles[b], items[b], splits_of(seq_of(a, b)));
     }
     a.tile_table[at] = e;
   }
 }
+
+// What a unit of keys (128 of the stream kernel, 64 of the tile kernel) takes a workgroup
+// that has its CU to itself, and a CU whose slots are full, in us: from chunks of 16 to
+// 1024 tokens after 1500 to 16000 keys, unsplit on few CUs and on all.  A split's sums are
+// written and read at kSumBytesPerUs, its join takes kJoinUs beside.
+struct Pace {
+  float alone, full;
+};
+constexpr Pace kPace[2][3] = {{{0.71f, 0.48f}, {0.95f, 0.85f}, {1.24f, 1.24f}},   // 32 rows; dim 64, 128, 256
+                              {{0.82f, 0.64f}, {1.09f, 1.07f}, {1.99f, 2.10f}}};  // 128 rows
+constexpr double kBytesPerUs = 5.2e6, kSumBytesPerUs = 1.2e6, kJoinUs = 4.;
 
 AttnArgs plan(const eb_attention_op &o) {
   AttnArgs a{};
@@ -123,26 +143,80 @@ AttnArgs plan(const eb_attention_op &o) {
     const int64_t packed = (int64_t)o.rows * a.group / tile_rows + o.batch;
     return o.batch > 1 && packed < each ? packed : each;
   };
-  a.tile_rows = rows <= 32 || tiles_of(128) * heads < cus ? 32 : 128;
-  const int64_t tiles = tiles_of(a.tile_rows);
-  a.part_rows = (int32_t)(rows < a.tile_rows ? rows : a.tile_rows);
-  // Splits of the keys: where the tiles alone leave workgroup slots idle, or one
-  // sequence of a batch may be far longer than the others.
-  // (workgroups on a CU: see kStreamWgs and the tile kernel's launch bounds)
-  const int64_t slots = cus * (o.cache.dim == 256 ? 1 : o.cache.dim == 64 && a.tile_rows == 32 ? 3 : 2);
-  a.unit = a.tile_rows == 32 ? 128 : 64;
-  a.min_units = a.tile_rows == 32 ? 1 : 16;
-  int64_t see = o.max_kv;
-  if (o.window > 0 && o.mask != EB_MASK_FULL && !o.prefix && see > (int64_t)o.window + a.tile_rows)
-    see = (int64_t)o.window + a.tile_rows;
-  const int64_t units = (see + a.unit - 1) / a.unit;
-  if (tiles * heads * 2 <= slots ? units > a.min_units : o.batch > 1 && units > 16) {
-    const int64_t target = (slots + heads - 1) / heads;
-    a.target = (int32_t)(target < kMaxSplits ? target : kMaxSplits);
+  // Kernel and splits: the least time by the paces above, of the two kernels, each
+  // without splits and with the number of pieces whose sums cost least.  Tiles of 32 rows
+  // are shorter and more, those of 128 read keys from L2 and LDS a quarter as often, and
+  // splits pay where tiles are few and keys many.  Measured, causal, 8 key/value and 32
+  // query heads of 128, us (32 rows whole, in pieces; 128 rows whole, in pieces):
+  //   256 tokens, no others      9.3   19    12.0    -        chosen: 9.3
+  //   2048 tokens, no others     69    81    53      65       52.7
+  //   1 token, 8000 keys         60    15.8   -      -        15.8
+  //   64 tokens, 1500 keys       18.0  15.6  33.3    20.2     15.6
+  //   256 tokens, 16000 keys     137   104   273     85       88
+  //   1024 tokens, 16000 keys    337   337   285     261      290
+  double best = 0.;
+  for (int32_t tile_rows = 32; tile_rows <= (rows <= 32 ? 32 : 128); tile_rows += 96) {
+    const Pace pace = kPace[tile_rows == 128][o.cache.dim / 128];
+    const int64_t tiles = tiles_of(tile_rows), unit = tile_rows == 32 ? 128 : 64;
+    const int32_t part_rows = (int32_t)(rows < tile_rows ? rows : tile_rows);
+    int64_t see = o.max_kv > 0 ? o.max_kv : 1;
+    double mean = (double)see - (o.mask == EB_MASK_FULL || o.prefix ? 0. : 0.5 * max_new);  // keys of a row
+    if (o.window > 0 && o.mask != EB_MASK_FULL && !o.prefix && see > (int64_t)o.window + tile_rows)
+      see = (int64_t)o.window + tile_rows;
+    if (mean > see) mean = (double)see;
+    if (mean < 1.) mean = 1.;
+    if (o.batch > 1) mean *= 0.5;  // (lengths are known to the GPU alone)
+    const double slots = (double)(cus * (o.cache.dim == 256 ? 1 : o.cache.dim == 64 && tile_rows == 32 ? 3 : 2));
+    const double wgs = (tiles - 0.5 * (o.batch - 1)) * heads, units = (double)((see + unit - 1) / unit);
+    // of the CUs together, and of the longest tile
+    const double compute = wgs * mean / unit * pace.full / cus;
+    const double memory = (double)o.batch * heads * mean * o.cache.dim * 4. / kBytesPerUs;
+    const double work = compute > memory ? compute : memory;
+    const double shared = 0.75 * pace.full * (wgs < slots ? wgs : slots) / cus;
+    const double longest = units * (shared > pace.alone ? shared : pace.alone);
+    // (several sequences: the longest may begin when others have ended.  Single tokens of
+    // 64 sequences of 30 to 16000 keys: 272 us whole, 152 in pieces; of 4000 keys each: 185,
+    // 191 with a join that finds nothing to do.)
+    const double whole = o.batch > 1 ? work + 0.5 * longest : work > longest ? work : longest;
+    // With splits: pieces of all tiles, each of which writes its sums once.
+    const double sums = part_rows * (o.cache.dim + 2) * 4. / kSumBytesPerUs;
+    const double all = (o.batch > 1 ? wgs * mean / unit : wgs * units) * pace.alone;
+    double pieces = slots;
+    if (pieces * pieces * sums > all) pieces = __builtin_sqrt(all / sums);
+    // (one workgroup a CU reaches the copy rate: 131071 keys of one head of 256, 256 pieces
+    // 35 us, 97 of them 43; of 128, 256 pieces 21.9 us, 512 of them 24.7)
+    if (o.batch == 1 && memory > compute && pieces > cus) pieces = (double)cus;
+    int64_t target = (int64_t)(pieces / heads);
+    if (target > kMaxSplits) target = kMaxSplits;
+    if (tile_rows == 128 && target > tiles * kJoinRows) target = tiles * kJoinRows;
+    if (o.batch == 1) target = target / tiles * tiles;  // the same number of splits for all
+    double split = whole + 1.;
+    if (target > (o.batch > 1 ? 0 : tiles)) {
+      const double piece = all / (target * heads);
+      split = (work > piece ? work : piece) + kJoinUs + target * heads * sums;
+    }
+    const double time = split < whole ? split : whole;
+    if (tile_rows > 32 && time >= best) break;
+    best = time;
+    a.tile_rows = tile_rows;
+    a.unit = (int32_t)unit;
+    a.min_units = tile_rows == 32 ? 1 : 4;  // (16 tokens, 1500 keys: with 16 units 34 us, 14.4)
+    a.part_rows = part_rows;
+    a.tiles = (uint32_t)tiles;
+    a.target = split < whole ? (int32_t)target : 0;
+    a.join_splits = (int32_t)(o.batch > 1 ? target : target / tiles);
   }
-  a.tiles = (uint32_t)tiles;
-  a.spread = rows <= a.tile_rows;
-  a.items = (uint32_t)(tiles + a.target);
+  // (half of what a CU gets on average: single tokens of 128 sequences of 30 to 4000 keys,
+  // 99 us, with 1.25 of it 104; to 1500 keys, 56 and 54)
+  a.even = 0.6f * (float)heads / (float)cus;
+  a.join_tiles = a.target < (int64_t)a.tiles ? a.target : (int32_t)a.tiles;
+  a.items = o.batch > 1 ? a.tiles + (uint32_t)a.target : a.target > 0 ? (uint32_t)a.target : a.tiles;
+  // In order over the XCDs, or a run of neighbours to each: single tiles share no keys;
+  // under a causal mask or of ragged sequences, runs are of unequal work unless each XCD
+  // gets whole heads (causal, 4096 tokens, one head of 256: 126 us spread, 185 in runs;
+  // 8 heads of 128: 148 either way).
+  a.spread = rows <= a.tile_rows ||
+             (heads % 8 != 0 && (o.batch > 1 || (a.target == 0 && o.mask != EB_MASK_FULL && !o.prefix)));
   const int64_t grid = (int64_t)a.items * heads;
   a.grid = (uint32_t)grid;
   a.grid_wgs = (uint32_t)((grid + 7) / 8 * 8);
@@ -159,7 +233,7 @@ static size_t sums_bytes(const AttnArgs &a) {
 }
 
 static size_t table_bytes(const AttnArgs &a) {
-  return a.o.batch > kScanBatch ? ((size_t)a.items + a.tiles + 15) / 16 * 16 * sizeof(int4) : 0;
+  return a.o.batch > kScanBatch ? ((size_t)a.items + a.join_tiles + 15) / 16 * 16 * sizeof(int4) : 0;
 }
 
 size_t attention_ws_bytes(const eb_attention_op &o) {

@@ -17,6 +17,7 @@ struct Item {
   int32_t p0 = 0;         // place of the first new token
   int32_t kv = 0;
   int32_t rows = 0;       // of the tile
+  uint32_t tiles = 0;     // of the sequence
   int32_t tok0 = 0, head0 = 0;  // of the tile's first row
 };
 
@@ -41,17 +42,19 @@ __device__ inline Seq seq_of(const AttnArgs &a, int32_t b) {
   return s;
 }
 
-// Units of a split, of `units` units in all tiles of several sequences: so that
-// the splits of all together are about a.target.
-__device__ inline uint32_t units_per_split(const AttnArgs &a, float units) {
+// Units of a split, of `units` units in all tiles of several sequences, `longest` of
+// them in one: so that the splits of all together are about a.target, and none where
+// the tiles are so alike that the GPU is busy to their end.
+__device__ inline uint32_t units_per_split(const AttnArgs &a, float units, int32_t longest) {
   // exact below 2^24
   const uint32_t per = units < 16777216.f ? ((uint32_t)units + a.target - 1) / a.target
                                           : (uint32_t)(units / a.target) + 2;
-  return max(per, (uint32_t)a.min_units);
+  return max(max(per, (uint32_t)a.min_units), (float)longest <= a.even * units ? (uint32_t)longest : 0u);
 }
 
-// Item number `at` of a key/value head: the sequences' row tiles in order, each
-// `splits` times (JOIN: once, and *base is its first item).  One sequence is
+// Item number `at` of a key/value head.  A sequence's items are the tiles of its first
+// split, those of its second and so on, so that neighbours read the same keys.  JOIN: item
+// `at` of the tiles with several splits, *base the item of its first split.  One sequence is
 // split as often as fits a.target items; of several, each into splits of
 // units_per_split units, so that a longer one gets more.  Every wave of every
 // workgroup finds the same numbers from the lengths; of more than kScanBatch
@@ -73,7 +76,7 @@ __device__ inline Item find_item(const AttnArgs &a, uint32_t at, uint32_t *base 
         splits = (s.units + per - 1) / per;
       }
     }
-    if (at >= s.tiles * (JOIN ? 1 : splits)) return it;
+    if (at >= s.tiles * (JOIN ? 1 : splits) || (JOIN && splits == 1)) return it;
     it.b = 0;
     it.splits = uni(splits);
   } else if (o.batch > kScanBatch) {
@@ -82,26 +85,31 @@ __device__ inline Item find_item(const AttnArgs &a, uint32_t at, uint32_t *base 
     if (it.b < 0) return it;
     s = seq_of(a, it.b);
     it.splits = max(uni(e.w), 1);
-    rest = JOIN ? e.y : e.y * it.splits + e.z;
-    first = JOIN ? e.z - e.y * it.splits : 0;
+    rest = JOIN ? e.y : e.z * s.tiles + e.y;
+    first = JOIN ? e.z : 0;
   } else {
     uint32_t per = 1;
     if (a.target > 0) {
       float units = 0.f;
+      int32_t longest = 0;
       if (lane < o.batch) {
         s = seq_of(a, lane);
         units = (float)s.tiles * (float)s.units;
+        longest = s.tiles > 0 ? s.units : 0;
       }
 #pragma unroll
-      for (int d = 32; d >= 1; d >>= 1) units += __shfl_xor(units, d);
-      per = units_per_split(a, units);
+      for (int d = 32; d >= 1; d >>= 1) {
+        units += __shfl_xor(units, d);
+        longest = max(longest, __shfl_xor(longest, d));
+      }
+      per = units_per_split(a, units, longest);
     }
     uint32_t items = 0, tiles = 0;
     if (lane < o.batch) {
       if (a.target <= 0) s = seq_of(a, lane);  // (else it is here already)
       splits = a.target > 0 && s.units > 0 ? (s.units + per - 1) / per : 1;
-      tiles = s.tiles;
-      items = tiles * splits;
+      items = s.tiles * splits;
+      tiles = splits > 1 ? s.tiles : 0;
     }
     uint32_t sum = items, count = tiles;
 #pragma unroll
@@ -123,20 +131,22 @@ __device__ inline Item find_item(const AttnArgs &a, uint32_t at, uint32_t *base 
     it.splits = from(splits);
     it.b = src;
   }
-  const uint32_t r = uni(rest), tile = JOIN ? r : r / it.splits;
-  it.split = JOIN ? 0 : (int32_t)(r - tile * it.splits);
-  if (JOIN) *base = first + r * it.splits;
+  const uint32_t tiles = uni(s.tiles), r = uni(rest), split = JOIN ? 0 : r / max(tiles, 1u);
+  const uint32_t tile = r - split * tiles;
+  it.split = (int32_t)split;
+  it.tiles = tiles;
+  if (JOIN) *base = first;
   it.q0 = uni(s.q0);
   it.n = uni(s.n);
   it.p0 = uni(s.p0);
   it.kv = uni(s.kv);
   // Under a causal mask the last tile of one sequence sees most keys and begins first
   // (4096 x 4096, 24 heads: 157 -> 134 us; in ragged batches it cost 2 us of 18).
-  const uint32_t tiles = uni(s.tiles);
-  if (tile >= tiles) {  // (offsets that are none: sequences that overlap without end)
+  if (tile >= tiles || it.split >= it.splits) {  // (offsets that are none: sequences that overlap without end)
     it.b = -1;
     return it;
   }
+  if (JOIN) *base += tile;
   const uint32_t row0 = (o.batch > 1 || o.mask == EB_MASK_FULL ? tile : tiles - 1 - tile) * a.tile_rows;
   it.rows = min(a.tile_rows, (int32_t)(it.n * a.group - row0));
   it.tok0 = uni(row0 / a.group);

