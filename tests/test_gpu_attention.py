@@ -581,3 +581,53 @@ def test_other_stream(eb):
         got = [eb.attention(q, *args) for _ in range(3)]
     s.synchronize()
     assert all(torch.equal(g, want) for g in got)
+
+
+# One sequence, and batches, whose keys are split between workgroups: max_new and max_kv
+# bound more than is there, as in a captured graph, and the kernel, its tiles and the
+# number of splits follow from them.
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("seqs,hq,hkv,max_new,max_kv,mask,prefix,window,cap", [
+    ([(40, 2600)], 8, 2, 40, 16000, "causal", None, 0, 0.0),
+    ([(40, 2600)], 8, 1, 300, 60000, "full", None, 0, 20.0),
+    ([(130, 1500)], 8, 1, 130, 16000, "causal", None, 0, 0.0),
+    ([(60, 1100)], 32, 8, 300, 16000, "causal", None, 0, 0.0),
+    ([(60, 1111)], 32, 8, 600, 64000, "causal", [1090], 0, 5.0),
+    ([(90, 1100)], 16, 2, 600, 64000, "causal", None, 900, 0.0),
+    ([(33, 700)], 64, 8, 50, 100000, "full", None, 0, 0.0),
+    ([(30, 1500), (1, 2500), (0, 9), (7, 40)], 16, 8, 30, 16000, "causal", None, 0, 0.0),
+    ([(40, 300), (9, 9), (1, 1100), (13, 800), (2, 2)], 32, 8, 40, 16000, "causal", [0, 3, 0, 795, 1], 0, 0.0),
+    ([(1, 30)] * 40 + [(3, 3000), (0, 4)] + [(5, 20)] * 30, 8, 2, 40, 60000, "causal", None, 0, 0.0),
+    ([(1, 16)] * 69 + [(1, 9000)], 8, 2, 1, 60000, "causal", None, 0, 0.0)])
+def test_attn_splits(eb, d, seqs, hq, hkv, max_new, max_kv, mask, prefix, window, cap):
+    new, lens = [n for n, _ in seqs], [t for _, t in seqs]
+    k, v, table = A.paged(lens, 16, hkv, d, BF, seed=d)
+    q = (_randn(sum(new) + 3, hq, d, seed=d + 1) * 1.5).to(BF)
+    q_start, kv_len = A.starts(new), A.ints(lens)
+    pre = A.ints(prefix) if prefix is not None else None
+    out = torch.full_like(q, 7.0)
+    eb.attention(q, eb.KVCache(k, v), table, q_start, kv_len, max_new, max_kv, mask, pre, window, cap, out=out)
+    torch.cuda.synchronize()
+    ref, err = A.attn_ref(q, k, v, table, q_start, kv_len, mask, prefix, window, cap)
+    A.assert_attn(out, ref, err, str(seqs[:4]), untouched=7.0)
+
+
+@pytest.mark.parametrize("d,hq,hkv,max_new,max_kv", [
+    (64, 8, 1, 40, 16000), (128, 8, 1, 40, 16000), (256, 8, 1, 40, 16000), (64, 32, 8, 300, 16000),
+    (128, 32, 8, 300, 16000), (256, 32, 8, 600, 64000)])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+def test_attn_splits_masked_places_hold_anything(eb, d, hq, hkv, max_new, max_kv, bad):
+    """The last 20 places of one sequence hold no numbers: tokens before them see none of it."""
+    new, kv = 40, 1100
+    k, v, table = A.paged([kv], 16, hkv, d, BF, seed=d)
+    for p in range(kv - 20, kv):
+        page = int(table[0, p // 16])
+        k[page, :, p % 16] = bad
+        v[page, :, p % 16] = bad
+    q = _randn(new, hq, d, seed=d + 1).to(BF)
+    q_start, kv_len = A.starts([new]), A.ints([kv])
+    out = eb.attention(q, eb.KVCache(k, v), table, q_start, kv_len, max_new, max_kv)
+    ref, err = A.attn_ref(q, k, v, table, q_start, kv_len)
+    assert bool(torch.isnan(ref[20:]).all()) and bool(torch.isfinite(ref[:20]).all())
+    A.assert_attn(out, ref, err, "before the last 20 places")
+    assert not bool(torch.isfinite(out[20:].float()).any())
