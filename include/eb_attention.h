@@ -188,7 +188,8 @@ typedef struct {
 
 /* Bytes of workspace eb_attention needs for *op: the fp32 sums of rows whose
  * keys are split over workgroups.  0 when it needs none or *op is invalid.
- * Depends on sizes, types and mask alone, not on device contents. Host-only
+ * Depends on sizes, types, mask, window and whether there is a prefix, not on
+ * device contents. Host-only
  * but for the current device's CU count. */
 size_t eb_attention_workspace_bytes(const eb_attention_op *op);
 

@@ -710,7 +710,7 @@ def attention(q: torch.Tensor, cache: KVCache, table: torch.Tensor, q_start: tor
         _check(_launch(_attention, op, dev, workspace.data_ptr(), workspace.numel()), "eb_attention")
         return out
     # its size, by what it depends on, is kept after a call that succeeded
-    key = (rows, batch, q_heads, cache.heads, dim, max_new, max_kv, dev)
+    key = (rows, batch, q_heads, cache.heads, dim, max_new, max_kv, mask, prefix is None, window, dev)
     nbytes = _ATTN_WS_BYTES.get(key)
     known = nbytes is not None
     if not known:
@@ -734,11 +734,13 @@ def attention(q: torch.Tensor, cache: KVCache, table: torch.Tensor, q_start: tor
 
 
 def attention_workspace_bytes(q_shape, cache: KVCache, batch: int, table_stride: int, max_new: int,
-                              max_kv: int) -> int:
-    """Bytes of workspace that attention() needs for queries of q_shape."""
+                              max_kv: int, mask: str = "causal", prefix: bool = False,
+                              window: int = 0) -> int:
+    """Bytes of workspace that attention() needs for queries of q_shape, with or
+    without a prefix, under this mask and window."""
     rows, q_heads, dim = q_shape
     w, stand_in = q_heads * dim, cache.k.data_ptr()  # pointers are only checked for alignment
     op = _PACK_ATTN.pack(stand_in, stand_in, *cache.shape, stand_in, stand_in, stand_in, stand_in,
-                         stand_in, 0, w, w, rows, batch, q_heads, table_stride, max_new, max_kv,
-                         EB_MASK_CAUSAL, 0, 1.0, 0.0)
+                         stand_in, stand_in if prefix else 0, w, w, rows, batch, q_heads, table_stride,
+                         max_new, max_kv, MASKS[mask], window, 1.0, 0.0)
     return int(_launch(_attention_ws, op, cache.index))

@@ -631,3 +631,28 @@ def test_attn_splits_masked_places_hold_anything(eb, d, hq, hkv, max_new, max_kv
     assert bool(torch.isnan(ref[20:]).all()) and bool(torch.isfinite(ref[:20]).all())
     A.assert_attn(out, ref, err, "before the last 20 places")
     assert not bool(torch.isfinite(out[20:].float()).any())
+
+
+def test_attn_workspace_of_each_mask(eb):
+    """Calls of the same sizes under other masks and windows, in either order: each takes
+    the workspace that it needs, its own or the caller's."""
+    kinds = [("causal", None, 100), ("causal", None, 0), ("full", None, 0), ("causal", [30], 0), ("full", None, 64),
+             ("causal", [30], 100)]
+    for order in (kinds, kinds[::-1]):
+        eb._ATTN_WS_BYTES.clear()
+        k, v, table = A.paged([300], 16, 2, 128, BF, seed=3)
+        cache, q = eb.KVCache(k, v), _randn(40, 8, 128, seed=4).to(BF)
+        q_start, kv_len = A.starts([40]), A.ints([300])
+        needs = set()
+        for mask, prefix, window in order:
+            pre = A.ints(prefix) if prefix else None
+            got = eb.attention(q, cache, table, q_start, kv_len, 40, 16000, mask, pre, window)
+            n = eb.attention_workspace_bytes(q.shape, cache, 1, table.shape[1], 40, 16000, mask, pre is not None,
+                                             window)
+            needs.add(n)
+            ws = torch.empty(max(n, 1), dtype=torch.uint8, device=DEV)
+            again = eb.attention(q, cache, table, q_start, kv_len, 40, 16000, mask, pre, window, workspace=ws)
+            ref, err = A.attn_ref(q, k, v, table, q_start, kv_len, mask, prefix, window)
+            A.assert_attn(got, ref, err, f"{mask} {prefix} {window}")
+            assert torch.equal(got, again)
+        assert 0 in needs and len(needs) > 1
