@@ -581,7 +581,7 @@ __device__ inline uint32_t missing_of(const Pages &pg, int32_t k0, int32_t kv, i
 
 // Many rows: 128 of a tile, 32 to each wave, all waves over the same keys, which
 // are copied to LDS ahead of their use (one barrier a tile).  Bound by the matrix
-// cores: 4096 tokens that all see each other, 24 heads of 128, bf16: 201 us, 1.02
+// cores: 4096 tokens that all see each other, 24 heads of 128, bf16: 200 us, 1.03
 // PFLOP/s, where a plain 8192^3 product of the same type reaches 1.19; 45% of cycles
 // issue MFMA, LDS is as busy, the rest is softmax beside them.  Heads of 256 (tiles of
 // 32 keys, one wave a SIMD) 950 TFLOP/s, of 64 (twice the softmax a product) 830.
