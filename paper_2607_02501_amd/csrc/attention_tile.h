@@ -771,6 +771,9 @@ __global__ void __launch_bounds__(256, kStreamWgs<D>) attn_stream_kernel(AttnArg
   static_assert(2 * kTile == 32 * D * 4, "a wave's tiles and its sums take the same room");
   __shared__ __attribute__((aligned(1024))) uint8_t lds[4 * 2 * kTile];
   __shared__ float2 ml[4][32];
+  __shared__ float4 factor[32];  // of the waves' sums of a row
+  __shared__ float2 total[32];   // a row's maximum and sum; or 1 / sum twice
+  __shared__ int64_t place[32];  // a row's first element in `out`
   __shared__ uint32_t again;
   const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   int32_t kh;
@@ -859,35 +862,52 @@ __global__ void __launch_bounds__(256, kStreamWgs<D>) attn_stream_kernel(AttnArg
   __syncthreads();
   const bool split = it.splits > 1;
   const int64_t item = (int64_t)kh * a.items + at;
-  const float4 *all = reinterpret_cast<const float4 *>(lds);
-  for (int32_t e = threadIdx.x; e < it.rows * (D / 4); e += 256) {
-    const int32_t rr = e / (D / 4), ch = e % (D / 4);
-    float mx = -INFINITY, l = 0.f;
+  if (threadIdx.x < 32) {
+    // what a row's elements share, once a row (by each thread for itself, a chunk took 0.5
+    // us longer with D = 128, 1 us with 256)
+    float mx = -INFINITY, l = 0.f, f[4];
 #pragma unroll
-    for (int u = 0; u < 4; ++u) mx = fmaxf(mx, ml[u][rr].x);
-    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int u = 0; u < 4; ++u) mx = fmaxf(mx, ml[u][threadIdx.x].x);
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
-      const float2 x = ml[u][rr];
+      const float2 x = ml[u][threadIdx.x];
       // (a wave that saw nothing has sums of 0, or NaN, which stays)
-      const float f = x.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(x.x - mx);
-      const float4 y = all[u * (8 * D) + rr * (D / 4) + (ch ^ (rr & 7))];
-      l = __builtin_fmaf(x.y, f, l);
-      v.x = __builtin_fmaf(y.x, f, v.x);
-      v.y = __builtin_fmaf(y.y, f, v.y);
-      v.z = __builtin_fmaf(y.z, f, v.z);
-      v.w = __builtin_fmaf(y.w, f, v.w);
+      f[u] = x.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(x.x - mx);
+      l = __builtin_fmaf(x.y, f[u], l);
     }
-    if (!((v.x + v.y + v.z + v.w + l) * 0.f == 0.f)) atomicOr(&again, 1u << rr);
-    int32_t tk, hd;
-    const int64_t rw = row_of(a, it, rr, kh, tk, hd);
+    factor[threadIdx.x] = make_float4(f[0], f[1], f[2], f[3]);
+    const float inv = l != 0.f ? 1.f / l : 0.f;
+    total[threadIdx.x] = split ? make_float2(mx, l) : make_float2(inv, inv);
+    if (live && !(l * 0.f == 0.f)) atomicOr(&again, 1u << threadIdx.x);
+    place[threadIdx.x] = row * a.o.out_stride + (int64_t)head * D;
+  }
+  __syncthreads();
+  const float4 *all = reinterpret_cast<const float4 *>(lds);
+#pragma unroll 2
+  for (int32_t e = threadIdx.x; e < it.rows * (D / 4); e += 256) {
+    const int32_t rr = e / (D / 4), ch = e % (D / 4);
+    const float4 f = factor[rr];
+    const float2 t = total[rr];
+    const float4 *const part = all + rr * (D / 4) + (ch ^ (rr & 7));
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+    auto add = [&](int u, float w) __attribute__((always_inline)) {
+      const float4 y = part[u * (8 * D)];
+      v.x = __builtin_fmaf(y.x, w, v.x);
+      v.y = __builtin_fmaf(y.y, w, v.y);
+      v.z = __builtin_fmaf(y.z, w, v.z);
+      v.w = __builtin_fmaf(y.w, w, v.w);
+    };
+    add(0, f.x);
+    add(1, f.y);
+    add(2, f.z);
+    add(3, f.w);
+    if (!((v.x + v.y + v.z + v.w) * 0.f == 0.f)) atomicOr(&again, 1u << rr);
     if (split) {
       *reinterpret_cast<float4 *>(part_o(a, item, rr, D) + 4 * ch) = v;
-      if (ch == 0) *part_ml(a, item, rr, D) = make_float2(mx, l);
+      if (ch == 0) *part_ml(a, item, rr, D) = t;
     } else {
-      const float inv = l != 0.f ? 1.f / l : 0.f;
-      *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(a.o.out) + rw * a.o.out_stride + (int64_t)hd * D + 4 * ch) =
-          make_uint2(pack2<T>(v.x * inv, v.y * inv), pack2<T>(v.z * inv, v.w * inv));
+      *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(a.o.out) + place[rr] + 4 * ch) =
+          make_uint2(pack2<T>(v.x * t.x, v.y * t.x), pack2<T>(v.z * t.x, v.w * t.x));
     }
   }
   __syncthreads();
