@@ -1072,10 +1072,11 @@ hipError_t attn_launch_d(const AttnArgs &a, hipStream_t s) {
   if (e != hipSuccess || a.target <= 0) return e;
   // one workgroup for each 1024 / D rows, or, of many splits, for each 64 elements of a
   // row, while that is not far more than run at once (one token, 131071 keys: one
-  // workgroup 91 us, its 32 parts 36; 256 tokens, 4000 keys: 39 us with 2048, 48 with 8192)
+  // workgroup 91 us, its 32 parts 36; 32 tokens of 2000 keys each, where nothing is split:
+  // 56.0 us with 1024, 57.7 with 2048; 256 tokens, 4000 keys: 39 with 2048, 48 with 8192)
   const uint32_t tiles = (uint32_t)(a.join_tiles * a.o.cache.heads), rows = (uint32_t)a.part_rows;
   const uint32_t parts = a.join_splits <= kJoinRows ? (rows * D + 1023) / 1024 : rows * (D / 64);
-  const uint32_t most = (2048 + tiles - 1) / tiles;
+  const uint32_t most = (1024 + tiles - 1) / tiles;
   attn_join_kernel<T, D><<<dim3(tiles, parts < most ? parts : most), 256, 0, s>>>(a);
   return hipGetLastError();
 }
