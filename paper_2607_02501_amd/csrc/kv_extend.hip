@@ -22,31 +22,33 @@ namespace eb {
 namespace {
 
 constexpr int kThreads = 512;
-constexpr int32_t kMost = 1 << 30;  // sums stop here: past any number of rows or pages
+// Sums stop here: past any number of rows or pages.  Two of them still fit 32 bits
+// without a sign, not with one.
+constexpr uint32_t kMost = 1u << 30;
 
 __device__ inline int64_t nonneg(int32_t v) { return v > 0 ? v : 0; }
-__device__ inline int32_t add_most(int32_t a, int32_t b) { return min(a + b, kMost); }
+__device__ inline uint32_t add_most(uint32_t a, uint32_t b) { return min(a + b, kMost); }
 
 // Inclusive sums (rows, pages), each at most kMost, over the workgroup's threads;
 // *total is that of all.
-__device__ inline int2 block_scan(int2 v, int2 *red, int2 *total) {
+__device__ inline uint2 block_scan(uint2 v, uint2 *red, uint2 *total) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
 #pragma unroll
   for (int d = 1; d < 64; d <<= 1) {
-    const int32_t x = __shfl_up(v.x, d), y = __shfl_up(v.y, d);
-    if (lane >= d) v = make_int2(add_most(v.x, x), add_most(v.y, y));
+    const uint32_t x = __shfl_up(v.x, d), y = __shfl_up(v.y, d);
+    if (lane >= d) v = make_uint2(add_most(v.x, x), add_most(v.y, y));
   }
   if (lane == 63) red[wave] = v;
   __syncthreads();
-  int2 before = make_int2(0, 0), all = make_int2(0, 0);
+  uint2 before = make_uint2(0, 0), all = make_uint2(0, 0);
 #pragma unroll
   for (int w = 0; w < kThreads / 64; ++w) {
-    const int2 u = red[w];
-    if (w < wave) before = make_int2(add_most(before.x, u.x), add_most(before.y, u.y));
-    all = make_int2(add_most(all.x, u.x), add_most(all.y, u.y));
+    const uint2 u = red[w];
+    if (w < wave) before = make_uint2(add_most(before.x, u.x), add_most(before.y, u.y));
+    all = make_uint2(add_most(all.x, u.x), add_most(all.y, u.y));
   }
   *total = all;
-  return make_int2(add_most(v.x, before.x), add_most(v.y, before.y));
+  return make_uint2(add_most(v.x, before.x), add_most(v.y, before.y));
 }
 
 __global__ void __launch_bounds__(kThreads) kv_extend_kernel(eb_kv_extend_op o, int page_shift) {
@@ -54,44 +56,44 @@ __global__ void __launch_bounds__(kThreads) kv_extend_kernel(eb_kv_extend_op o, 
   int32_t *start = lds;                // [batch + 1], at most o.rows
   int32_t *taken = lds + o.batch + 1;  // [batch + 1], at most kMost
   int32_t *cached = taken + o.batch + 1;
-  __shared__ int2 red[2][kThreads / 64];
+  __shared__ uint2 red[2][kThreads / 64];
   __shared__ int64_t lost;
   const int32_t page = o.page;
   const int64_t capacity = (int64_t)o.table_stride << page_shift;  // tokens of a table row
   const bool first = blockIdx.x == 0;
   const int32_t n_free = min(max(o.n_free[0], 0), o.free_capacity);
 
-  int2 before = make_int2(0, 0);
+  uint2 before = make_uint2(0, 0);
   for (int32_t b0 = 0; b0 < o.batch; b0 += kThreads) {
     const int32_t b = b0 + (int32_t)threadIdx.x;
     const bool ok = b < o.batch;
     const int64_t have = ok ? nonneg(o.cached[b]) : 0, add = ok ? nonneg(o.added[b]) : 0;
     const int64_t total = min(have + add, capacity), held = (min(have, capacity) + page - 1) >> page_shift;
-    const int32_t need = ok ? (int32_t)(((total + page - 1) >> page_shift) - held) : 0;
-    const int32_t rows = (int32_t)min(add, (int64_t)o.rows + 1);
-    int2 all;
+    const uint32_t need = ok ? (uint32_t)(((total + page - 1) >> page_shift) - held) : 0;
+    const uint32_t rows = (uint32_t)min(add, (int64_t)o.rows + 1);
+    uint2 all;
     // (the two halves of red in turn: one barrier a chunk of sequences)
-    const int2 in = block_scan(make_int2(rows, need), red[(b0 / kThreads) & 1], &all);
+    const uint2 in = block_scan(make_uint2(rows, need), red[(b0 / kThreads) & 1], &all);
     if (ok) {
       // (rows <= 2^24 + 1 and need <= 2^26 of a sequence, so a sum that stopped at kMost
       // less its own part is still past every row and every page of the stack)
-      start[b] = min(add_most(before.x, in.x - rows), o.rows);
-      taken[b] = add_most(before.y, in.y - need);
+      start[b] = (int32_t)min(add_most(before.x, in.x - rows), (uint32_t)o.rows);
+      taken[b] = (int32_t)add_most(before.y, in.y - need);
       cached[b] = (int32_t)have;
       if (first) {
         o.q_start[b] = start[b];
         o.kv_len[b] = (int32_t)total;
       }
     }
-    before = make_int2(add_most(before.x, all.x), add_most(before.y, all.y));
+    before = make_uint2(add_most(before.x, all.x), add_most(before.y, all.y));
   }
   if (threadIdx.x == 0) {
-    start[o.batch] = min(before.x, o.rows);
-    taken[o.batch] = before.y;
+    start[o.batch] = (int32_t)min(before.x, (uint32_t)o.rows);
+    taken[o.batch] = (int32_t)before.y;
     lost = 0;
     if (first) {
       o.q_start[o.batch] = start[o.batch];
-      o.n_free_out[0] = max(n_free - before.y, 0);
+      o.n_free_out[0] = max(n_free - (int32_t)before.y, 0);
     }
   }
   __syncthreads();
