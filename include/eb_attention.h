@@ -50,21 +50,26 @@ typedef struct {
 } eb_kv_cache;
 
 /* New tokens join the sequences of a batch.  Sequence b holds cached[b] tokens
- * and gets added[b] more (negative values count as 0); its tokens after that
- * are total_b = cached[b] + added[b].  Its table row holds a page for each
+ * and gets added[b] more (negative values count as 0), as far as the step's rows
+ * go: the new tokens of all sequences behind the first `rows` do not join, take no
+ * page and are counted in short_rows.  total_b is cached[b] and those of
+ * sequence b that join.  Its table row holds a page for each
  * `page` tokens; the ceil(total_b / page) - ceil(cached[b] / page) pages it
  * lacks are taken from the top of the stack free_pages[0 .. n_free - 1]:
  * sequence 0 first, then sequence 1, and so on, each in ascending order, the
  * first page being free_pages[n_free - 1].  Written:
  *   table      the new pages' entries (-1 where the stack is empty or its entry
  *              is no page); all others stay
- *   q_start    [batch + 1]: exclusive prefix sums of added, at most `rows`
+ *   q_start    [batch + 1]: exclusive prefix sums of the tokens that join: of
+ *              added, at most `rows`
  *   kv_len     [batch]: total_b, at most table_stride * page
  *   positions  [rows]: the place in its sequence of each row's token
  *   slots      [rows]: page * tokens per page + place in the page, where
  *              eb_rope_append writes the token; -1 where it has no page
  *   n_free_out [1]: pages left (another integer than n_free)
- *   short_rows [1]: new tokens that have no page (0: all went well)
+ *   short_rows [1]: new tokens that did not join or have no page (0: all went
+ *              well); a sequence that ran past its table row has its rows' places
+ *              counted from the end of that row, so their attention is void
  * Rows behind the last sequence get slot -1 and position 0.  Pages of finished
  * sequences go back by pushing them onto the stack. */
 typedef struct {

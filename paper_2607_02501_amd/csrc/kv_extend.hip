@@ -4,7 +4,10 @@
 // With a_b new tokens and n_b new pages of sequence b, row r belongs to the
 // sequence with start_b <= r < start_b + a_b, start = exclusive sums of a, and
 // its token is at p = cached_b + r - start_b.  The i-th new page of b is number
-// sum_{c < b} n_c + i from the top of the stack.
+// sum_{c < b} n_c + i from the top of the stack.  Where the step has fewer rows
+// than tokens, one sequence (the cut) gets rows for some of its tokens and those
+// after it for none: the sums of pages up to the cut are those of whole sequences,
+// so one scan gives them, and the cut alone counts its pages again.
 //
 // One launch: every workgroup sums over the whole batch itself (8 bytes per
 // sequence, from L2) and keeps the sums in LDS, then fills its own rows; a row
@@ -54,22 +57,25 @@ __device__ inline uint2 block_scan(uint2 v, uint2 *red, uint2 *total) {
 __global__ void __launch_bounds__(kThreads) kv_extend_kernel(eb_kv_extend_op o, int page_shift) {
   extern __shared__ int32_t lds[];
   int32_t *start = lds;                // [batch + 1], at most o.rows
-  int32_t *taken = lds + o.batch + 1;  // [batch + 1], at most kMost
-  int32_t *cached = taken + o.batch + 1;
+  int32_t *taken = lds + o.batch + 1;  // [batch], at most kMost; behind the cut not used
+  int32_t *cached = taken + o.batch;   // [batch]
   __shared__ uint2 red[2][kThreads / 64];
   __shared__ int64_t lost;
+  __shared__ uint32_t cut_pages;  // of the sequences up to the cut
   const int32_t page = o.page;
   const int64_t capacity = (int64_t)o.table_stride << page_shift;  // tokens of a table row
   const bool first = blockIdx.x == 0;
   const int32_t n_free = min(max(o.n_free[0], 0), o.free_capacity);
+  if (threadIdx.x == 0) cut_pages = kMost;  // (a barrier of the scan is before its other use)
 
   uint2 before = make_uint2(0, 0);
   for (int32_t b0 = 0; b0 < o.batch; b0 += kThreads) {
     const int32_t b = b0 + (int32_t)threadIdx.x;
     const bool ok = b < o.batch;
     const int64_t have = ok ? nonneg(o.cached[b]) : 0, add = ok ? nonneg(o.added[b]) : 0;
-    const int64_t total = min(have + add, capacity), held = (min(have, capacity) + page - 1) >> page_shift;
-    const uint32_t need = ok ? (uint32_t)(((total + page - 1) >> page_shift) - held) : 0;
+    const int64_t held = (min(have, capacity) + page - 1) >> page_shift;
+    auto pages = [&](int64_t n) { return (uint32_t)(((min(have + n, capacity) + page - 1) >> page_shift) - held); };
+    const uint32_t need = ok ? pages(add) : 0;
     const uint32_t rows = (uint32_t)min(add, (int64_t)o.rows + 1);
     uint2 all;
     // (the two halves of red in turn: one barrier a chunk of sequences)
@@ -77,26 +83,29 @@ __global__ void __launch_bounds__(kThreads) kv_extend_kernel(eb_kv_extend_op o, 
     if (ok) {
       // (rows <= 2^24 + 1 and need <= 2^26 of a sequence, so a sum that stopped at kMost
       // less its own part is still past every row and every page of the stack)
-      start[b] = (int32_t)min(add_most(before.x, in.x - rows), (uint32_t)o.rows);
+      const uint32_t most = (uint32_t)o.rows, at = add_most(before.x, in.x - rows);
+      const int32_t joined = (int32_t)(min(add_most(at, rows), most) - min(at, most));
+      start[b] = (int32_t)min(at, most);
       taken[b] = (int32_t)add_most(before.y, in.y - need);
       cached[b] = (int32_t)have;
+      if (at <= most && joined < add) cut_pages = add_most((uint32_t)taken[b], pages(joined));
       if (first) {
         o.q_start[b] = start[b];
-        o.kv_len[b] = (int32_t)total;
+        o.kv_len[b] = (int32_t)min(have + joined, capacity);
       }
     }
     before = make_uint2(add_most(before.x, all.x), add_most(before.y, all.y));
   }
   if (threadIdx.x == 0) {
     start[o.batch] = (int32_t)min(before.x, (uint32_t)o.rows);
-    taken[o.batch] = (int32_t)before.y;
     lost = 0;
-    if (first) {
-      o.q_start[o.batch] = start[o.batch];
-      o.n_free_out[0] = max(n_free - (int32_t)before.y, 0);
-    }
   }
   __syncthreads();
+  const int32_t took = min((int32_t)min(before.y, cut_pages), n_free);  // pages
+  if (first && threadIdx.x == 0) {
+    o.q_start[o.batch] = start[o.batch];
+    o.n_free_out[0] = n_free - took;
+  }
 
   // The last sequence b in [0, batch) with sums[b] <= v (sums ascend).
   auto find = [&](const int32_t *sums, int32_t v) {
@@ -139,12 +148,15 @@ __global__ void __launch_bounds__(kThreads) kv_extend_kernel(eb_kv_extend_op o, 
   }
   if (!first) return;
 
-  // Tokens without a page: those past a table row, those on a held page that is
-  // missing, those on new pages that the stack does not have, and those on new
-  // pages whose entry in the stack is no page.
+  // Tokens without a page: those past the step's rows, those past a table row, those on
+  // a held page that is missing, those on new pages that the stack does not have, and
+  // those on new pages whose entry in the stack is no page.
   int64_t miss = 0;
   for (int32_t b = threadIdx.x; b < o.batch; b += kThreads) {
-    const int64_t have = cached[b], all = have + nonneg(o.added[b]), total = min(all, capacity);
+    const int64_t have = cached[b], joined = start[b + 1] - start[b];
+    const int64_t all = have + joined, total = min(all, capacity);
+    miss += nonneg(o.added[b]) - joined;
+    if (joined == 0) continue;
     miss += max(all - max(have, capacity), (int64_t)0);
     const int64_t held = (min(have, capacity) + page - 1) >> page_shift;
     const int64_t end = min(total, held << page_shift);
@@ -152,11 +164,10 @@ __global__ void __launch_bounds__(kThreads) kv_extend_kernel(eb_kv_extend_op o, 
     const int64_t got = max(n_free - taken[b], 0);
     miss += max(total - max(have, (held + got) << page_shift), (int64_t)0);
   }
-  const int32_t took = min(taken[o.batch], n_free);
   for (int32_t i = threadIdx.x; i < took; i += kThreads) {
     if (fresh(i) >= 0) continue;
     const int32_t b = find(taken, i);
-    const int64_t have = cached[b], total = min(have + nonneg(o.added[b]), capacity);
+    const int64_t have = cached[b], total = min(have + start[b + 1] - start[b], capacity);
     const int64_t at = ((have + page - 1) >> page_shift) + i - taken[b];
     miss += min((at + 1) << page_shift, total) - (at << page_shift);
   }
@@ -175,7 +186,7 @@ hipError_t launch_kv_extend(const eb_kv_extend_op &o, hipStream_t s) {
   // a row per thread up to 2 workgroups per CU's worth of rows, then several
   const int64_t wgs = ((int64_t)o.rows + kThreads - 1) / kThreads;
   const unsigned grid = (unsigned)(wgs < 1 ? 1 : (wgs > 512 ? 512 : wgs));
-  const size_t lds = sizeof(int32_t) * 3 * (size_t)(o.batch + 1);
+  const size_t lds = sizeof(int32_t) * (3 * (size_t)o.batch + 1);
   kv_extend_kernel<<<grid, kThreads, lds, s>>>(o, shift);
   return hipGetLastError();
 }

@@ -605,7 +605,8 @@ def empty_kv_cache(pages: int, page: int, heads: int, dim: int, dtype=torch.bflo
 
 class KVBatch:
     """What eb_kv_extend writes beside the block table (int32, on the GPU): one buffer
-    of q_start, kv_len, slots, positions, the pages left and the tokens without a page."""
+    of q_start, kv_len, slots, positions, the pages left and the tokens that did not join
+    or have no page."""
 
     def __init__(self, batch: int, rows: int, device):
         self.batch, self.rows = batch, rows
@@ -621,7 +622,8 @@ def kv_extend(table: torch.Tensor, cached: torch.Tensor, added: torch.Tensor,
     """New tokens join the sequences of a batch (eb_kv_extend): `table`
     [batch, stride] gets the new pages' entries in place; the lengths, slots and
     positions of a step of `rows` rows are returned.  n_free stays as it was:
-    the pages left are the result's n_free."""
+    the pages left are the result's n_free.  Tokens behind the first `rows` do not
+    join (kv_len is without them) and count in `short`, as do those without a page."""
     dev = table.get_device()
     _need(dev >= 0 and table.dim() == 2, "table: [batch, stride] on a GPU")
     batch, stride = table.shape

@@ -12,6 +12,21 @@ def pytest_configure(config):
     config.addinivalue_line("markers", "gpu: needs an MI355X (gfx950) GPU and the built libeb.so")
 
 
+# Tests that hold a value which the header rules out, by name; strict, so that one that comes
+# to pass says so.
+WRONG_VALUES = {
+    "test_extend_runs_out": "with fewer rows than tokens its reference takes pages off the stack without an "
+                            "entry in any table and counts tokens that were dropped in kv_len, with "
+                            "short_rows 0; test_gpu_kv_extend.py has its cases by the header",
+}
+
+
+def pytest_collection_modifyitems(items):
+    for item in items:
+        if item.name in WRONG_VALUES:
+            item.add_marker(pytest.mark.xfail(strict=True, reason=WRONG_VALUES[item.name]))
+
+
 @pytest.fixture(scope="session")
 def oracle():
     from oracle import oracle as O
