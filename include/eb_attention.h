@@ -165,7 +165,8 @@ eb_status eb_rope_append(const eb_rope_append_op *op, hipStream_t stream);
  * maxima and sums of the softmax are fp32; capped scores are off by at most
  * softcap * 2^-20, which is why caps past 2^10 are not taken.  The weights e^{t - max} are rounded
  * once to the cache's type for the second product (each off by at most 2^-8 of
- * itself for EB_BF16, 2^-11 for EB_F16), as is the output.
+ * itself for EB_BF16, 2^-11 for EB_F16, or 2^-36 of the row's largest weight, where
+ * that is more), as is the output.
  * With several sequences, or few rows, the keys of a row are split over
  * workgroups and joined in a fixed order by a second launch: results are
  * deterministic. */

@@ -16,10 +16,15 @@
 // no score changes lanes.
 //
 // Softmax.  One pass, with a running maximum m and sum l per row in fp32; p =
-// 2^((s - m) c).  m is raised, and O and l rescaled, only when a row's maximum
-// has grown by more than a factor 2^8 in p: p then stays below 2^8, and most
-// tiles skip the rescale.  p enters the product rounded to the cache's type (its
-// sum l takes p itself).
+// 2^((s - m) c + lift).  m is raised, and O and l rescaled, only when a row's
+// maximum has grown by more than a factor 2^late in p: p then stays below
+// 2^(late + lift), and most tiles skip the rescale.  p enters the product rounded to
+// the cache's type, since the matrix cores take two 16-bit operands (its sum l takes p
+// itself).  bfloat16 has fp32's exponents: late 8, lift 0.  binary16 ends at 2^16 and
+// has fewer bits below 2^-14: late 4, lift 11, so that a weight of 2^-25 of the
+// row's largest is still a normal number, where without a lift one of 2^-14 was the
+// last and one of 2^-26 was 0.  The lift is in O, l and the maximum that goes
+// with them, so it cancels.
 //
 // Masks.  The keys a row sees are one interval; a tile that lies inside every
 // row's interval skips the comparisons.  Keys past the sequence's end and on
@@ -185,6 +190,8 @@ struct Wave {
   int32_t any_lo, any_hi;  // and that some row sees
   bool masked;           // a tile was compared
 
+  static constexpr float kLift = T == EB_F16 ? 11.f : 0.f, kLate = T == EB_F16 ? 4.f : 8.f;
+
   __device__ void begin() {
 #pragma unroll
     for (int b = 0; b < kBlocks; ++b) o[b] = f32x16_t(0.f);
@@ -298,7 +305,7 @@ struct Wave {
       top = top_of(s);
     }
     top = row_max(top);
-    if (__ballot((top - m) * c > 8.f)) {
+    if (__ballot((top - m) * c > kLate)) {
       const float to = fmaxf(m, top);
       const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m - to) * c);
       m = to;
@@ -309,7 +316,9 @@ struct Wave {
   }
 
   // What settled scores' exponents start from, and a pair's weights.
-  __device__ float base_of(const AttnArgs &a) const { return m == -INFINITY ? 0.f : CAP ? -m : -m * a.scale2; }
+  __device__ float base_of(const AttnArgs &a) const { return m == -INFINITY ? 0.f : -top_exponent(a); }
+  // O and l are sums of 2^(t - this), t being a score times c.
+  __device__ float top_exponent(const AttnArgs &a) const { return __builtin_fmaf(m, CAP ? 1.f : a.scale2, -kLift); }
   __device__ uint32_t pair(const AttnArgs &a, float base, float x, float y) {
     const float c = CAP ? 1.f : a.scale2;
     const float u = __builtin_amdgcn_exp2f(__builtin_fmaf(x, c, base));
@@ -508,8 +517,8 @@ __device__ inline void row_again(const AttnArgs &a, const uint16_t *qrow, int64_
 // kernels
 // ---------------------------------------------------------------------------
 
-// Sums of a split: D values of each row of the tile, and its maximum (times c) and
-// sum.
+// Sums of a split: D values of each row of the tile, the exponent that they are above
+// (Wave::top_exponent; of row_again's, its maximum times c) and their sum.
 __device__ inline float *part_o(const AttnArgs &a, int64_t item, int32_t row, int d) {
   return a.ws + (item * a.part_rows + row) * d;
 }
@@ -705,7 +714,7 @@ __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) attn_tile_kernel(AttnAr
         for (int i = 0; i < 16; i += 4)
           *reinterpret_cast<float4 *>(dst + 32 * b + 8 * (i / 4) + 4 * half) =
               make_float4(w.o[b][i], w.o[b][i + 1], w.o[b][i + 2], w.o[b][i + 3]);
-      if (half == 0) *part_ml(a, item, 32 * wv + (lane & 31), D) = make_float2(w.m * c, w.l);
+      if (half == 0) *part_ml(a, item, 32 * wv + (lane & 31), D) = make_float2(w.top_exponent(a), w.l);
     } else {
       uint16_t *dst = static_cast<uint16_t *>(a.o.out) + row * a.o.out_stride + (int64_t)head * D;
       const float inv = w.l != 0.f ? 1.f / w.l : 0.f;
@@ -851,7 +860,7 @@ __global__ void __launch_bounds__(256, kStreamWgs<D>) attn_stream_kernel(AttnArg
   // 4 c .. 4 c + 3 of row r of a wave are chunk c ^ (r % 8) of row r of its part.
   const float c = CAP ? 1.f : a.scale2;
   const int r = lane & 31, half = lane >> 5;
-  if (half == 0) ml[wv][r] = make_float2(w.m * c, w.l);
+  if (half == 0) ml[wv][r] = make_float2(w.top_exponent(a), w.l);
   if (threadIdx.x == 0) again = 0;
   float4 *const sums = reinterpret_cast<float4 *>(mine) + r * (D / 4);
 #pragma unroll
