@@ -14,6 +14,7 @@ from __future__ import annotations
 import ctypes
 import os
 import struct
+import threading
 
 import torch
 
@@ -225,22 +226,31 @@ def from_canonical(blocks: torch.Tensor, qtype: str, n: int, k: int) -> QWeights
     return out
 
 
-_SCRATCH = {}
+class _Scratch(threading.local):
+    """Workspaces of direct calls, by device and stream.  A thread has its own: a call is
+    several launches, and those of two threads on one stream (torch's default for every
+    thread) may fall between each other's, since ctypes lets go of the interpreter."""
+
+    def __init__(self):
+        self.bufs = {}
+
+
+_SCRATCH = _Scratch()
 
 
 def scratch(device, nbytes: int):
     """A caller-owned workspace of at least nbytes on `device` for direct calls
-    on the current stream (one growing torch buffer per device and stream;
-    calls on one stream run in order, so they may share it)."""
+    on the current stream (one growing torch buffer per thread, device and stream;
+    a thread's calls on one stream run in order, so they may share it)."""
     if nbytes <= 0:
         return None
     device = torch.device(device)
     key = (device.index if device.index is not None else torch.cuda.current_device(),
            _stream(device))
-    buf = _SCRATCH.get(key)
+    buf = _SCRATCH.bufs.get(key)
     if buf is None or buf.numel() < nbytes:
         buf = torch.empty(max(nbytes, 4 << 20), dtype=torch.uint8, device=device)
-        _SCRATCH[key] = buf
+        _SCRATCH.bufs[key] = buf
     return buf
 
 
@@ -284,7 +294,7 @@ def _run_op(qw: QWeights, x: torch.Tensor, out: torch.Tensor, x_type: int, path:
     if not known:
         nbytes = _ws_bytes(op, path)
     if nbytes:
-        ws = _SCRATCH.get((dev, stream))
+        ws = _SCRATCH.bufs.get((dev, stream))
         if ws is None or ws.numel() < nbytes:
             ws = scratch(x.device, nbytes)
         st = _fused_ws(op, path, ws.data_ptr(), ws.numel(), stream)
@@ -723,7 +733,7 @@ def attention(q: torch.Tensor, cache: KVCache, table: torch.Tensor, q_start: tor
         if _capturing():
             ws = torch.empty(nbytes, dtype=torch.uint8, device=cache.device)
         else:
-            ws = _SCRATCH.get((dev, _raw_stream(dev)))
+            ws = _SCRATCH.bufs.get((dev, _raw_stream(dev)))
             if ws is None or ws.numel() < nbytes:
                 ws = scratch(cache.device, nbytes)
         st = _launch(_attention, op, dev, ws.data_ptr(), ws.numel())
