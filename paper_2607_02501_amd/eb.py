@@ -575,6 +575,18 @@ _get_device = torch._C._cuda_getDevice
 _capturing = torch._C._cuda_isCurrentStreamCapturing
 
 
+def _capturing_on(dev: int) -> bool:
+    """Whether GPU `dev`'s current stream is being captured."""
+    was = _get_device()
+    if was == dev:
+        return _capturing()
+    torch.cuda.set_device(dev)
+    try:
+        return _capturing()
+    finally:
+        torch.cuda.set_device(was)
+
+
 def _launch(fn, op: bytes, dev: int, *more) -> int:
     """fn(op, *more, stream) with GPU `dev` current, on its current stream."""
     was = _get_device()
@@ -730,7 +742,7 @@ def attention(q: torch.Tensor, cache: KVCache, table: torch.Tensor, q_start: tor
     if not nbytes:
         st = _launch(_attention, op, dev, None, 0)
     else:
-        if _capturing():
+        if _capturing_on(dev):
             ws = torch.empty(nbytes, dtype=torch.uint8, device=cache.device)
         else:
             ws = _SCRATCH.bufs.get((dev, _raw_stream(dev)))

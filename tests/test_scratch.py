@@ -62,3 +62,14 @@ def test_threads_have_a_workspace_each(calls, monkeypatch):
     for t in threads:
         t.join(30)
     assert len(seen) == 2 and len(set(seen.values())) == 2
+
+
+def test_capture_on_another_device_than_the_current(calls, monkeypatch):
+    """A captured call's workspace belongs to the graph, whichever device is current."""
+    eb, current = calls.eb, [0]
+    monkeypatch.setattr(eb, "_get_device", lambda: current[0])
+    monkeypatch.setattr(torch.cuda, "set_device", lambda d: current.__setitem__(0, d))
+    monkeypatch.setattr(eb, "_capturing", lambda: current[0] == -1)
+    calls.call()
+    assert not eb._SCRATCH.bufs and current == [0]
+    assert calls.got[0][1] == 1000
