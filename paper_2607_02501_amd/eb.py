@@ -238,20 +238,43 @@ class _Scratch(threading.local):
 _SCRATCH = _Scratch()
 
 
+_get_device = torch._C._cuda_getDevice
+_capturing = torch._C._cuda_isCurrentStreamCapturing
+
+
+def _capturing_on(dev: int) -> bool:
+    """Whether GPU `dev`'s current stream is being captured."""
+    was = _get_device()
+    if was == dev:
+        return _capturing()
+    torch.cuda.set_device(dev)
+    try:
+        return _capturing()
+    finally:
+        torch.cuda.set_device(was)
+
+
+def _workspace(device, dev: int, stream: int, nbytes: int) -> torch.Tensor:
+    """scratch() of GPU `dev`'s current stream."""
+    if _capturing_on(dev):
+        return torch.empty(nbytes, dtype=torch.uint8, device=device)
+    bufs = _SCRATCH.bufs
+    buf = bufs.get((dev, stream))
+    if buf is None or buf.numel() < nbytes:
+        buf = bufs[dev, stream] = torch.empty(max(nbytes, 4 << 20), dtype=torch.uint8, device=device)
+    return buf
+
+
 def scratch(device, nbytes: int):
     """A caller-owned workspace of at least nbytes on `device` for direct calls
     on the current stream (one growing torch buffer per thread, device and stream;
-    a thread's calls on one stream run in order, so they may share it)."""
+    a thread's calls on one stream run in order, so they may share it).  Under graph
+    capture a fresh one, of the graph's memory: graphs may run at the same time."""
     if nbytes <= 0:
         return None
     device = torch.device(device)
-    key = (device.index if device.index is not None else torch.cuda.current_device(),
-           _stream(device))
-    buf = _SCRATCH.bufs.get(key)
-    if buf is None or buf.numel() < nbytes:
-        buf = torch.empty(max(nbytes, 4 << 20), dtype=torch.uint8, device=device)
-        _SCRATCH.bufs[key] = buf
-    return buf
+    dev = device.index if device.index is not None else torch.cuda.current_device()
+    return _workspace(device, dev, _stream(device), nbytes)
 
 
 def _run_tuned(op: eb_qlinear_op, device, tile: int, splits: int) -> None:
@@ -294,9 +317,7 @@ def _run_op(qw: QWeights, x: torch.Tensor, out: torch.Tensor, x_type: int, path:
     if not known:
         nbytes = _ws_bytes(op, path)
     if nbytes:
-        ws = _SCRATCH.bufs.get((dev, stream))
-        if ws is None or ws.numel() < nbytes:
-            ws = scratch(x.device, nbytes)
+        ws = _workspace(x.device, dev, stream, nbytes)
         st = _fused_ws(op, path, ws.data_ptr(), ws.numel(), stream)
     else:
         st = _fused_ws(op, path, None, 0, stream)
@@ -571,22 +592,6 @@ def _heads(name: str, t: torch.Tensor, dev: int, dtype, rows: int, heads: int, d
     return stride if rows > 1 else heads * dim
 
 
-_get_device = torch._C._cuda_getDevice
-_capturing = torch._C._cuda_isCurrentStreamCapturing
-
-
-def _capturing_on(dev: int) -> bool:
-    """Whether GPU `dev`'s current stream is being captured."""
-    was = _get_device()
-    if was == dev:
-        return _capturing()
-    torch.cuda.set_device(dev)
-    try:
-        return _capturing()
-    finally:
-        torch.cuda.set_device(was)
-
-
 def _launch(fn, op: bytes, dev: int, *more) -> int:
     """fn(op, *more, stream) with GPU `dev` current, on its current stream."""
     was = _get_device()
@@ -709,8 +714,7 @@ def attention(q: torch.Tensor, cache: KVCache, table: torch.Tensor, q_start: tor
     """Attention of a batch's new tokens over the paged cache (eb_attention):
     q [rows, q_heads, dim] -> the same shape.  scale: dim ** -0.5 where not
     given.  workspace: a uint8 tensor of attention_workspace_bytes bytes; without
-    one the call takes one from scratch(), or, under graph capture, a fresh one
-    that belongs to the graph."""
+    one the call takes one from scratch()."""
     dev, dim = cache.index, cache.dim
     if q.dim() != 3 or table.dim() != 2:
         raise ValueError("q: [rows, q_heads, dim]; table: [batch, stride]")
@@ -742,12 +746,7 @@ def attention(q: torch.Tensor, cache: KVCache, table: torch.Tensor, q_start: tor
     if not nbytes:
         st = _launch(_attention, op, dev, None, 0)
     else:
-        if _capturing_on(dev):
-            ws = torch.empty(nbytes, dtype=torch.uint8, device=cache.device)
-        else:
-            ws = _SCRATCH.bufs.get((dev, _raw_stream(dev)))
-            if ws is None or ws.numel() < nbytes:
-                ws = scratch(cache.device, nbytes)
+        ws = _workspace(cache.device, dev, _raw_stream(dev), nbytes)
         st = _launch(_attention, op, dev, ws.data_ptr(), ws.numel())
     _check(st, "eb_attention")
     if not known:

@@ -73,3 +73,30 @@ def test_capture_on_another_device_than_the_current(calls, monkeypatch):
     calls.call()
     assert not eb._SCRATCH.bufs and current == [0]
     assert calls.got[0][1] == 1000
+
+
+def test_captured_projections_have_a_workspace_each(calls, monkeypatch):
+    """Two graphs captured on one stream may run at the same time."""
+    eb, got, kept = calls.eb, [], []
+    qw = SimpleNamespace(qtype="q8_0", n=64, k=64, buf=torch.zeros(64, dtype=torch.uint8))
+    x, out = torch.zeros(4, 64, dtype=torch.bfloat16), torch.zeros(4, 64)
+    empty = torch.empty
+
+    def keep(*args, **kw):   # the graph's memory outlives the call
+        kept.append(empty(*args, **kw))
+        return kept[-1]
+
+    def fused(op, path, ws, nbytes, stream):
+        got.append(ws)
+        return eb.EB_OK
+
+    monkeypatch.setattr(eb, "_ws_bytes", lambda op, path: 1000)
+    monkeypatch.setattr(eb, "_fused_ws", fused)
+    monkeypatch.setattr(eb, "_WS_BYTES", {})
+    monkeypatch.setattr(torch, "empty", keep)
+    for capturing in (False, True, True, False):
+        monkeypatch.setattr(eb, "_capturing", lambda: capturing)
+        eb._run_op(qw, x, out, eb.EB_BF16, eb.EB_PATH_AUTO)
+    assert got[0] == got[3] and len(set(got[:3])) == 3
+    monkeypatch.setattr(eb, "_capturing", lambda: True)
+    assert eb.scratch("cpu", 1000).data_ptr() != eb.scratch("cpu", 1000).data_ptr()
