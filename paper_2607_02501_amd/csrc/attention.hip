@@ -129,10 +129,11 @@ AttnArgs plan(const eb_attention_op &o) {
     a.scale2 = 2.f * kLog2e * o.scale / o.softcap;
     a.cap2 = o.softcap * kLog2e;
   } else {
-    // a negative scale is a sign on the queries; with a scale of 0 every score
-    // becomes 0 times a number that a hidden key's -infinity outweighs
+    // a negative scale is a sign on the queries; in place of a scale of 0, which would make
+    // NaN of a hidden key's -infinity, the least above it: no finite score times it is over
+    // 2^-21
     a.flip = o.scale < 0.f ? 0x80008000u : 0u;
-    a.scale2 = o.scale == 0.f ? 1e-30f : (o.scale < 0.f ? -o.scale : o.scale) * kLog2e;
+    a.scale2 = o.scale == 0.f ? 0x1p-149f : (o.scale < 0.f ? -o.scale : o.scale) * kLog2e;
   }
   const int64_t max_new = o.max_new < o.rows ? o.max_new : o.rows;
   const int64_t rows = max_new * a.group;  // of a sequence and key/value head

@@ -56,3 +56,16 @@ def test_attn_one_key_far_above_the_others(eb, dtype, gap, new, kv, hq, hkv, d, 
         size = float(v.float().abs().max()) * kv
         err = err + 2.0 ** -36 * size
     A.assert_attn(got, ref, err, f"gap {gap}")
+
+
+@pytest.mark.parametrize("scale", [0.0, -0.0])
+@pytest.mark.parametrize("new,kv,hq,hkv,cap", [(1, 300, 4, 2, 0.0), (130, 400, 64, 4, 0.0), (20, 900, 4, 2, 9.0)])
+def test_attn_scale_of_zero(eb, scale, new, kv, hq, hkv, cap):
+    """Every key that is seen has the same weight, however large its score would be."""
+    k, v, table = A.paged([kv], 16, hkv, 64, BF, seed=kv)
+    k.mul_(2.0 ** 50)
+    q = _randn(new, hq, 64, seed=2, dtype=BF) * 2.0 ** 50
+    q_start, kv_len = A.starts([new]), A.ints([kv])
+    got = eb.attention(q, eb.KVCache(k, v), table, q_start, kv_len, new, kv, softcap=cap, scale=scale)
+    ref, err = A.attn_ref(q, k, v, table, q_start, kv_len, softcap=cap, scale=scale)
+    A.assert_attn(got, ref, err, f"scale {scale}")
