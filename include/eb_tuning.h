@@ -3,12 +3,14 @@
  * eb.h: measuring the MFMA path's tile configurations and splits of k one by
  * one (paper section 3.2, backend-specific dispatch: the automatic choice of
  * eb_qlinear is a cost model over these configurations, checked against such
- * measurements).  No process-wide state: the choice is an argument per call.
+ * measurements), and telling which kernel attention takes.  No process-wide
+ * state: the choice is an argument per call.
  */
 #ifndef EB_TUNING_H
 #define EB_TUNING_H
 
 #include "eb.h"
+#include "eb_attention.h"
 
 #ifdef __cplusplus
 extern "C" {
@@ -28,6 +30,14 @@ int32_t eb_mfma_tile_count(void);
  * range. */
 eb_status eb_qlinear_tuned(const eb_qlinear_op *op, int32_t tile, int32_t splits, void *workspace,
                            size_t workspace_bytes, hipStream_t stream);
+
+/* What eb_attention launches for *op on the current device, without a launch: row tiles
+ * of *tile_rows rows (32: the kernel whose waves take keys in turn, 128: the one
+ * whose waves take rows and share key tiles), and *splits, the workgroups of a key/value
+ * head that splits of keys may add at most (0: none is split).  How often a tile is
+ * split follows from the lengths on the GPU.
+ * EB_ERR_INVALID: null pointer, or rows 0; else errors as eb_attention's for *op. */
+eb_status eb_attention_plan(const eb_attention_op *op, int32_t *tile_rows, int32_t *splits);
 
 #ifdef __cplusplus
 }

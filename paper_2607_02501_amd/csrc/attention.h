@@ -16,6 +16,7 @@ constexpr int kScanBatch = 64;    // sequences that every wave looks over itself
 hipError_t launch_kv_extend(const eb_kv_extend_op &o, hipStream_t s);
 hipError_t launch_rope_append(const eb_rope_append_op &o, hipStream_t s);
 size_t attention_ws_bytes(const eb_attention_op &o);
+void attention_plan(const eb_attention_op &o, int32_t *tile_rows, int32_t *splits);
 hipError_t launch_attention(const eb_attention_op &o, void *ws, hipStream_t s);
 
 // Splits of a tile up to which the join takes whole rows (attn_join_kernel): 7 splits of 50

@@ -242,6 +242,12 @@ size_t attention_ws_bytes(const eb_attention_op &o) {
   return sums_bytes(a) + table_bytes(a);
 }
 
+void attention_plan(const eb_attention_op &o, int32_t *tile_rows, int32_t *splits) {
+  const AttnArgs a = plan(o);
+  *tile_rows = a.tile_rows;
+  *splits = a.target;
+}
+
 hipError_t launch_attention(const eb_attention_op &o, void *ws, hipStream_t s) {
   AttnArgs a = plan(o);
   a.ws = static_cast<float *>(ws);

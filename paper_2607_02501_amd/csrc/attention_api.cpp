@@ -1,10 +1,12 @@
-// attention_api.cpp -- the C entry points of include/eb_attention.h: host-side
+// attention_api.cpp -- the C entry points of include/eb_attention.h (and eb_attention_plan
+// of include/eb_tuning.h): host-side
 // validation (before any HIP call, so that every error path runs without a GPU)
 // and the launchers' calls.
 #include <hip/hip_runtime.h>
 
 #include <cmath>
 
+#include "../../include/eb_tuning.h"
 #include "attention.h"
 
 namespace eb {
@@ -185,6 +187,15 @@ eb_status eb_rope_append(const eb_rope_append_op *op, hipStream_t stream) {
 size_t eb_attention_workspace_bytes(const eb_attention_op *op) {
   if (!op || check_attention(*op) != EB_OK || op->rows == 0) return 0;
   return attention_ws_bytes(*op);
+}
+
+eb_status eb_attention_plan(const eb_attention_op *op, int32_t *tile_rows, int32_t *splits) {
+  if (!op || !tile_rows || !splits) return EB_ERR_INVALID;
+  const eb_status st = check_attention(*op);
+  if (st != EB_OK) return st;
+  if (op->rows == 0) return EB_ERR_INVALID;
+  attention_plan(*op, tile_rows, splits);
+  return EB_OK;
 }
 
 eb_status eb_attention(const eb_attention_op *op, void *workspace, size_t workspace_bytes,

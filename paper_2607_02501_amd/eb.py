@@ -547,6 +547,8 @@ lib.eb_attention_workspace_bytes.restype = ctypes.c_size_t
 lib.eb_attention_workspace_bytes.argtypes = [ctypes.POINTER(eb_attention_op)]
 lib.eb_attention.restype = _i32
 lib.eb_attention.argtypes = [ctypes.POINTER(eb_attention_op), _vp, ctypes.c_size_t, _vp]
+lib.eb_attention_plan.restype = _i32
+lib.eb_attention_plan.argtypes = [_vp, ctypes.POINTER(_i32), ctypes.POINTER(_i32)]
 _kv_extend, _rope_append, _attention = _raw.eb_kv_extend, _raw.eb_rope_append, _raw.eb_attention
 for _f in (_kv_extend, _rope_append):
     _f.restype, _f.argtypes = _i32, [ctypes.c_char_p, _vp]
@@ -756,14 +758,29 @@ def attention(q: torch.Tensor, cache: KVCache, table: torch.Tensor, q_start: tor
     return out
 
 
+def _attention_sizes(q_shape, cache, batch, table_stride, max_new, max_kv, mask, prefix, window) -> bytes:
+    rows, q_heads, dim = q_shape
+    w, stand_in = q_heads * dim, cache.k.data_ptr()  # pointers are only checked for alignment
+    return _PACK_ATTN.pack(stand_in, stand_in, *cache.shape, stand_in, stand_in, stand_in, stand_in,
+                           stand_in, stand_in if prefix else 0, w, w, rows, batch, q_heads, table_stride,
+                           max_new, max_kv, MASKS[mask], window, 1.0, 0.0)
+
+
 def attention_workspace_bytes(q_shape, cache: KVCache, batch: int, table_stride: int, max_new: int,
                               max_kv: int, mask: str = "causal", prefix: bool = False,
                               window: int = 0) -> int:
     """Bytes of workspace that attention() needs for queries of q_shape, with or
     without a prefix, under this mask and window."""
-    rows, q_heads, dim = q_shape
-    w, stand_in = q_heads * dim, cache.k.data_ptr()  # pointers are only checked for alignment
-    op = _PACK_ATTN.pack(stand_in, stand_in, *cache.shape, stand_in, stand_in, stand_in, stand_in,
-                         stand_in, stand_in if prefix else 0, w, w, rows, batch, q_heads, table_stride,
-                         max_new, max_kv, MASKS[mask], window, 1.0, 0.0)
+    op = _attention_sizes(q_shape, cache, batch, table_stride, max_new, max_kv, mask, prefix, window)
     return int(_launch(_attention_ws, op, cache.index))
+
+
+def attention_plan(q_shape, cache: KVCache, batch: int, table_stride: int, max_new: int, max_kv: int,
+                   mask: str = "causal", prefix: bool = False, window: int = 0) -> tuple:
+    """(rows of a tile, workgroups that splits may add) of attention() on these sizes, for
+    tuning and tests (eb_attention_plan)."""
+    op = _attention_sizes(q_shape, cache, batch, table_stride, max_new, max_kv, mask, prefix, window)
+    tile_rows, splits = _i32(), _i32()
+    _check(_launch(lambda op, stream: lib.eb_attention_plan(op, tile_rows, splits), op, cache.index),
+           "eb_attention_plan")
+    return tile_rows.value, splits.value

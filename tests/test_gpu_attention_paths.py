@@ -69,3 +69,176 @@ def test_attn_scale_of_zero(eb, scale, new, kv, hq, hkv, cap):
     got = eb.attention(q, eb.KVCache(k, v), table, q_start, kv_len, new, kv, softcap=cap, scale=scale)
     ref, err = A.attn_ref(q, k, v, table, q_start, kv_len, softcap=cap, scale=scale)
     A.assert_attn(got, ref, err, f"scale {scale}")
+
+
+# ---------------------------------------------------------------------------
+# the kernel of 128-row tiles, whole and with its keys split: rows behind the last
+# sequence and bounds above the lengths choose it for sequences that are small
+# enough for the reference
+# ---------------------------------------------------------------------------
+
+# rows of q, max_new, max_kv
+ROOM = {"whole": (8000, 8000, 16000), "split": (500, 500, 60000)}
+
+
+def _tiles(eb, room, q, cache, table, q_start, kv_len, mask="causal", prefix=None, window=0, cap=0.0):
+    """attention() on 128-row tiles, which the plan is asked about first."""
+    rows, max_new, max_kv = ROOM[room] if isinstance(room, str) else room
+    wide = torch.zeros(rows, *q.shape[1:], dtype=q.dtype, device=DEV)
+    wide[:len(q)] = q
+    out = torch.full_like(wide, 7.0)
+    tile_rows, splits = eb.attention_plan(wide.shape, cache, len(kv_len), table.shape[1], max_new, max_kv, mask,
+                                          prefix is not None, window)
+    assert tile_rows == 128 and (splits > 0) == (room == "split" or room == RAGGED["split"]), (tile_rows, splits)
+    eb.attention(wide, cache, table, q_start, kv_len, max_new, max_kv, mask,
+                 A.ints(prefix) if prefix is not None else None, window, cap, out=out)
+    torch.cuda.synchronize()
+    assert bool((out[len(q):] == 7.0).all())
+    return out[:len(q)]
+
+
+RAGGED = {"whole": (8000, 8000, 1000), "split": (8000, 8000, 16000)}
+
+
+@pytest.mark.parametrize("room", ["whole", "split"])
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("dtype", [BF, FP])
+@pytest.mark.parametrize("new,kv,mask,prefix,window,cap", [
+    (150, 420, "causal", None, 0, 0.0), (150, 420, "causal", None, 0, 30.0), (129, 129, "causal", None, 0, 0.0),
+    (200, 333, "full", None, 0, 0.0), (150, 420, "causal", [390], 0, 20.0), (150, 420, "causal", [0], 21, 0.0),
+    (150, 420, "causal", [300], 64, 0.0), (150, 420, "full", None, 40, 5.0), (100, 40, "causal", [7], 0, 0.0),
+    (33, 1100, "causal", None, 0, 0.0), (1, 77, "full", None, 0, 0.0)])
+def test_tiles_masks(eb, room, d, dtype, new, kv, mask, prefix, window, cap):
+    hq, hkv = 8, 2
+    k, v, table = A.paged([kv], 16, hkv, d, dtype, seed=kv)
+    q = (_randn(new, hq, d, seed=new) * 1.5).to(dtype)
+    q_start, kv_len = A.starts([new]), A.ints([kv])
+    got = _tiles(eb, room, q, eb.KVCache(k, v), table, q_start, kv_len, mask, prefix, window, cap)
+    ref, err = A.attn_ref(q, k, v, table, q_start, kv_len, mask, prefix, window, cap)
+    A.assert_attn(got, ref, err, f"{new} {kv}")
+
+
+@pytest.mark.parametrize("d,window,kv", [(64, 200, 500), (128, 200, 500), (256, 700, 900)])
+@pytest.mark.parametrize("dtype", [BF, FP])
+def test_tiles_causal_window(eb, d, window, kv, dtype):
+    k, v, table = A.paged([kv], 32, 2, d, dtype, seed=d)
+    q = (_randn(150, 8, d, seed=d + 1) * 1.5).to(dtype)
+    q_start, kv_len = A.starts([150]), A.ints([kv])
+    got = _tiles(eb, "whole", q, eb.KVCache(k, v), table, q_start, kv_len, window=window)
+    ref, err = A.attn_ref(q, k, v, table, q_start, kv_len, window=window)
+    A.assert_attn(got, ref, err, f"window {window}")
+
+
+@pytest.mark.parametrize("room", ["whole", "split"])
+@pytest.mark.parametrize("many", [False, True])
+@pytest.mark.parametrize("d,page,dtype", [(64, 16, FP), (64, 64, BF), (128, 32, BF), (128, 128, FP), (256, 64, FP), (256, 16, BF)])
+def test_tiles_ragged(eb, room, many, d, page, dtype):
+    """Tiles of several sequences, of more than a wave looks over itself too; rows that see
+    nothing, tokens past the keys, sequences without tokens or keys."""
+    seqs = [(100, 100), (1, 40), (31, 500), (0, 7), (3, 2), (40, 1500), (2, 0), (15, 16), (200, 300)]
+    if many:
+        rng = np.random.default_rng(d)
+        seqs += [(int(rng.integers(0, 6)), int(rng.integers(0, 60))) for _ in range(81)]
+    new, lens = [n for n, _ in seqs], [t for _, t in seqs]
+    hq, hkv = 64, 2
+    k, v, table = A.paged(lens, page, hkv, d, dtype, seed=d + page)
+    q = (_randn(sum(new), hq, d, seed=d) * 1.5).to(dtype)
+    q_start, kv_len = A.starts(new), A.ints(lens)
+    prefix = [int(t) // 2 for t in lens]
+    got = _tiles(eb, RAGGED[room], q, eb.KVCache(k, v), table, q_start, kv_len, prefix=prefix)
+    ref, err = A.attn_ref(q, k, v, table, q_start, kv_len, prefix=prefix)
+    A.assert_attn(got, ref, err, "ragged")
+
+
+@pytest.mark.parametrize("room", ["whole", "split"])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), float("-inf"), 3e38])
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("dtype", [BF, FP])
+def test_tiles_masked_places_hold_anything(eb, room, bad, d, dtype):
+    """Places that a mask, a window, a missing page or the end of the sequence hides."""
+    new, kv, page, hq, hkv = 100, 330, 16, 8, 2
+    bad = 6e4 if dtype == FP and bad == 3e38 else bad
+    k, v, table = A.paged([kv], page, hkv, d, dtype, seed=5)
+    q = (_randn(new, hq, d, seed=6) * 1.5).to(dtype)
+    q_start, kv_len = A.starts([new]), A.ints([kv])
+    ids = table[0].cpu().long()
+
+    def spoil(c, places):
+        c, j = c.clone(), torch.as_tensor(places)
+        c[ids[j // page].to(DEV), :, (j % page).to(DEV)] = bad
+        return c
+
+    def run(ks, vs, t=table, prefix=None, window=0):
+        return _tiles(eb, room, q, eb.KVCache(ks, vs), t, q_start, kv_len, "causal", prefix, window)
+
+    clean = run(k, v)
+    ref, err = A.attn_ref(q, k, v, table, q_start, kv_len)
+    A.assert_attn(clean, ref, err, "clean")
+    # pages of nobody and places past the end
+    mine = torch.zeros(len(k), dtype=torch.bool)
+    mine[ids] = True
+    ks, vs = spoil(k, range(kv, len(ids) * page)), spoil(v, range(kv, len(ids) * page))
+    ks[~mine.to(DEV)], vs[~mine.to(DEV)] = bad, bad
+    assert torch.equal(run(ks, vs), clean)
+    # the last 20 places, of which the tokens before them see none
+    last = range(kv - 20, kv)
+    got = run(spoil(k, last), spoil(v, last))
+    A.assert_attn(got[:-20], ref[:-20], err[:-20], "before the last places")
+    got = run(k, spoil(v, last))
+    A.assert_attn(got[:-20], ref[:-20], err[:-20], "before the last places, values")
+    # the first 250 places, behind a window of 20: tokens at 270 and later see none
+    ks, vs = spoil(k, range(250)), spoil(v, range(250))
+    got = run(ks, vs, prefix=[0], window=20)
+    refw, errw = A.attn_ref(q, k, v, table, q_start, kv_len, prefix=[0], window=20)
+    A.assert_attn(got[40:], refw[40:], errw[40:], "window")
+    # their pages missing, and one in between
+    t = table.clone()
+    t[0, :16] = A.ints([-1, len(k), -2 ** 31, 2 ** 31 - 1] * 4)
+    t[0, 18] = -1
+    ks, vs = spoil(k, range(256)), spoil(v, range(256))
+    for c in (ks, vs):
+        c[ids[18]] = bad
+    refm, errm = A.attn_ref(q, k, v, t, q_start, kv_len)
+    A.assert_attn(run(ks, vs, t), refm, errm, "missing pages")
+
+
+@pytest.mark.parametrize("room", ["whole", "split"])
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("gap", [12, 16, 20])
+def test_tiles_one_key_far_above_the_others(eb, room, d, gap):
+    """As above, of the 128-row tiles, and joined where splits have different maxima."""
+    new, kv, hq, hkv = 70, 600, 8, 2
+    k, v, table = A.paged([kv], 64, hkv, d, FP, seed=kv)
+    k.zero_()
+    v.mul_(0.25).add_(1.0)
+    first = int(table[0, 0])
+    k[first, :, 0, 0], v[first, :, 0] = 1.0, 0.0
+    q = torch.zeros(new, hq, d, dtype=FP, device=DEV)
+    q[:, :, 0] = float(gap) * d ** 0.5
+    q_start, kv_len = A.starts([new]), A.ints([kv])
+    got = _tiles(eb, room, q, eb.KVCache(k, v), table, q_start, kv_len)
+    ref, err = A.attn_ref(q, k, v, table, q_start, kv_len)
+    A.assert_attn(got, ref, err + 2.0 ** -36 * float(v.float().abs().max()) * kv, f"gap {gap}")
+
+
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("dtype", [BF, FP])
+@pytest.mark.parametrize("new,hq,hkv,splits", [(1, 8, 1, True), (30, 8, 8, True), (5, 4, 4, False)])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+def test_few_rows_masked_places_hold_anything(eb, d, dtype, new, hq, hkv, splits, bad):
+    """Tiles of 32 rows, whole and split: rows computed again beside rows that are not."""
+    kv, page, max_kv = 1100, 16, 16000 if splits else 100
+    k, v, table = A.paged([kv], page, hkv, d, dtype, seed=d)
+    for p in list(range(kv - new + (new + 1) // 2, kv)) + list(range(300)):
+        k[int(table[0, p // page]), :, p % page] = bad
+        v[int(table[0, p // page]), :, p % page] = bad
+    q = (_randn(new, hq, d, seed=d + 1) * 1.5).to(dtype)
+    q_start, kv_len, prefix = A.starts([new]), A.ints([kv]), A.ints([0])
+    cache, window = eb.KVCache(k, v), kv - 300 - new
+    plan = eb.attention_plan(q.shape, cache, 1, table.shape[1], new, max_kv, "causal", True, window)
+    assert plan[0] == 32 and (plan[1] > 0) == splits, plan
+    got = eb.attention(q, cache, table, q_start, kv_len, new, max_kv, prefix=prefix, window=window)
+    ref, err = A.attn_ref(q, k, v, table, q_start, kv_len, prefix=[0], window=window)
+    live = (new + 1) // 2
+    assert bool(torch.isfinite(ref[:live]).all())
+    A.assert_attn(got[:live], ref[:live], err[:live], "rows that see numbers alone")
