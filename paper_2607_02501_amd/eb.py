@@ -256,7 +256,7 @@ def _capturing_on(dev: int) -> bool:
 
 def _workspace(device, dev: int, stream: int, nbytes: int) -> torch.Tensor:
     """scratch() of GPU `dev`'s current stream."""
-    if _capturing_on(dev):
+    if _capturing() if _get_device() == dev else _capturing_on(dev):
         return torch.empty(nbytes, dtype=torch.uint8, device=device)
     bufs = _SCRATCH.bufs
     buf = bufs.get((dev, stream))
