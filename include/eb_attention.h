@@ -24,7 +24,8 @@
  *     may cache rows that no visible key lives in.
  *   - Calls on one stream run in order; a workspace is used in stream order,
  *     so calls that share one must be ordered (two graphs that may run at the
- *     same time need one each).
+ *     same time need one each, and so do two host threads on one stream: a call
+ *     is up to three launches).
  */
 #ifndef EB_ATTENTION_H
 #define EB_ATTENTION_H
@@ -136,7 +137,8 @@ typedef struct {
   int32_t style;            /* EB_ROT_HALF or EB_ROT_ADJACENT */
   int32_t n_axes;           /* 1 .. 3 */
   int32_t sections[3];      /* each >= 0, those of the axes adding up to rot / 2 */
-  float norm_eps;           /* finite, >= 0 (a zero head needs eps > 0) */
+  float norm_eps;           /* finite, >= 0 (a zero head needs eps > 0; eps + the mean of squares,
+                               in fp32, is taken as 2^-126 at least) */
 } eb_rope_append_op;
 
 /* EB_ERR_INVALID: null pointer, a size, stride or enum out of range, an output
@@ -156,7 +158,8 @@ eb_status eb_rope_append(const eb_rope_append_op *op, hipStream_t stream);
  * keys and values already: with t_j = scale * q . k_j, capped to
  * softcap * tanh(t_j / softcap) where softcap > 0,
  *   out = sum_j e^{t_j} v_j / sum_j e^{t_j}      over the keys j that are seen.
- * A row that sees no key is 0; a key on a missing page is not seen.  Query head
+ * A row that sees no key is 0, and so is one whose scores are all -infinity, over
+ * finite values; a key on a missing page is not seen.  Query head
  * h reads key/value head h / (q_heads / heads).
  * max_new and max_kv are the host's bounds on any sequence's new tokens and
  * kv_len: they decide the launch; tokens past max_new are not computed (their

@@ -109,8 +109,12 @@ __global__ void __launch_bounds__(kItemThreads) attn_items_kernel(AttnArgs a) {
 
 // What a unit of keys (128 of the stream kernel, 64 of the tile kernel) takes a workgroup
 // that has its CU to itself, and a CU whose slots are full, in us: from chunks of 16 to
-// 1024 tokens after 1500 to 16000 keys, unsplit on few CUs and on all.  A split's sums are
-// written and read at kSumBytesPerUs, its join takes kJoinUs beside.
+// 1024 tokens after 1500 to 16000 keys, unsplit on few CUs and on all, causal and without a
+// cap.  A split's sums are written and read at kSumBytesPerUs, its join takes kJoinUs beside.
+// Outside that range they are extrapolated: 816 capped rows of 8 heads of 256 behind a
+// prefix, 8.7 us by these paces, take 19.  The factors in plan (half the bound of a batch's
+// lengths, 0.75 of a full CU's pace for tiles that share it, half the longest tile after the
+// rest) and `even` below are set by the cases named there and the ones in the table.
 struct Pace {
   float alone, full;
 };
@@ -154,7 +158,7 @@ AttnArgs plan(const eb_attention_op &o) {
   //   1 token, 8000 keys         60    15.8   -      -        15.8
   //   64 tokens, 1500 keys       18.0  15.6  33.3    20.2     15.6
   //   256 tokens, 16000 keys     137   104   273     85       88
-  //   1024 tokens, 16000 keys    337   337   285     261      290
+  //   1024 tokens, 16000 keys    337   337   285     261      290 (the estimate has it shorter)
   double best = 0.;
   for (int32_t tile_rows = 32; tile_rows <= (rows <= 32 ? 32 : 128); tile_rows += 96) {
     const Pace pace = kPace[tile_rows == 128][o.cache.dim / 128];

@@ -590,12 +590,14 @@ __device__ inline uint32_t missing_of(const Pages &pg, int32_t k0, int32_t kv, i
 
 // Many rows: 128 of a tile, 32 to each wave, all waves over the same keys, which
 // are copied to LDS ahead of their use (one barrier a tile).  Bound by the matrix
-// cores: 4096 tokens that all see each other, 24 heads of 128, bf16: 200 us, 1.03
-// PFLOP/s, where a plain 8192^3 product of the same type reaches 1.19; 45% of cycles
-// issue MFMA, LDS is as busy, the rest is softmax beside them.  Heads of 256 (tiles of
-// 32 keys, one wave a SIMD) 950 TFLOP/s, of 64 (twice the softmax a product) 830.
-// Causal: 134 us, half the work at 0.77 of the rate, since a tile's last key block is
-// half masked.
+// cores: 4096 tokens that all see each other, 24 heads of 128, bf16: 200 to 212 us, 0.97
+// to 1.03 PFLOP/s, where a plain 8192^3 product of the same type reaches 1.19; 45% of
+// cycles issue MFMA, LDS is as busy, the rest is softmax beside them.  Heads of 256 (tiles
+// of 32 keys, one wave a SIMD) 950 TFLOP/s, of 64 (twice the softmax a product) 830.
+// Causal: 134 us, half the work at 0.77 of the rate.  Half-masked key blocks are 3% of
+// it; the rest is uneven CUs: each XCD gets three heads of 32 tiles, each longest first,
+// so the first 64 items put the longest tiles of two heads on one CU, 128 units of 64 keys
+// where the mean CU has 99 (at 1.07 us a unit that is 137 us, and 106 if all had the mean).
 template <int T, int D, int BK, bool CAP>
 __global__ void __launch_bounds__(256, D == 256 ? 1 : 2) attn_tile_kernel(AttnArgs a) {
   constexpr int kTile = BK * D * 2;  // bytes of a tile of keys or values
@@ -767,10 +769,10 @@ constexpr int kStreamWgs = D == 64 ? 3 : 256 / D;
 // four waves' sums are joined in LDS at the end.  Of one tile or few a wave the
 // kernel is a chain of latencies, and fetching code that has not run yet is one of
 // them: the sums are joined in chunks of 16 bytes, a quarter of the code.
-// Measured: single tokens of 48 sequences, 456 MB of keys and values, 88 us (5.2 TB/s, a
-// large copy 5.14); one token after 131071 keys of 256, 134 MB, 24 us (5.6 TB/s); after
-// 900 of 32 heads, 6.4 us, of which 1.4 wait for lengths, 0.4 for the page table, 1.3 for
-// keys, 0.5 for values and 1 goes into the join in LDS.  Chunks are bound by the copies
+// Measured, means of 40 launches: single tokens of 48 sequences, 456 MB of keys and values,
+// 91 us (5.0 TB/s, a large copy 5.14); one token after 131071 keys of 256, 134 MB, 25.4 us
+// (5.3 TB/s); after 900 of 32 heads, 6.8 us, of which 1.4 wait for lengths, 0.4 for the page
+// table, 1.3 for keys, 0.5 for values and 1 goes into the join in LDS.  Chunks are bound by the copies
 // to LDS, which each wave makes for its 32 rows alone: 128 keys of 128 take 0.95 us on a
 // CU by itself, 65 KB which is 69 GB/s; a CU reads 126 from L2.
 template <int T, int D, bool CAP>

@@ -4,9 +4,9 @@
 // Per head x of d elements: y = x g / sqrt(eps + sum x^2 / d), then pairs
 // (a, b) -> (a cos t - b sin t, b cos t + a sin t), t = position * freq; values
 // are only copied.  Bound by bytes: QKV read once, queries, keys and values
-// written once.  4096 rows of 24 + 48 heads of 128, bf16, 151 MB: 28 us, 5.4 TB/s (a large
-// copy 5.14); 820 rows of 10 heads of 256, fp32 in, 12 MB: 5.6 us; one row: 3.4 us, a launch
-// and three dependent reads.
+// written once.  4096 rows of 24 + 48 heads of 128, bf16, 151 MB: 29.3 us, 5.15 TB/s (a large
+// copy 5.14; means of 40 launches); 820 rows of 10 heads of 256, fp32 in, 12 MB: 5.7 us; one
+// row: 3.5 us, a launch and three dependent reads.
 //
 // A lane holds 8 elements of a head: 4 rotated pairs, or 8 elements behind the
 // rotated part, so both halves of every pair are in one lane for either pair

@@ -1,5 +1,6 @@
-"""Attention over the paged cache at the numerical edges of its two kernels, on the GPU,
-against the 64-bit reference of tests/attention_helpers.py."""
+"""Attention over the paged cache in both of its kernels, and at the edges of its numbers
+and of the head norm's, on the GPU, against the 64-bit reference of
+tests/attention_helpers.py."""
 import numpy as np
 import pytest
 import torch
@@ -242,3 +243,36 @@ def test_few_rows_masked_places_hold_anything(eb, d, dtype, new, hq, hkv, splits
     live = (new + 1) // 2
     assert bool(torch.isfinite(ref[:live]).all())
     A.assert_attn(got[:live], ref[:live], err[:live], "rows that see numbers alone")
+
+
+# ---------------------------------------------------------------------------
+# ends of the ranges
+# ---------------------------------------------------------------------------
+
+@pytest.mark.parametrize("new,hq,hkv,max_new,max_kv,rows", [(1, 4, 2, 1, 40, 1), (30, 4, 2, 30, 16000, 30),
+                                                            (70, 8, 2, 8000, 16000, 8000)])
+def test_attn_scores_all_minus_infinity(eb, new, hq, hkv, max_new, max_kv, rows):
+    """Such a row is 0, as one that sees no key; beside a key with a score it takes that one's value."""
+    kv = 100
+    k, v, table = A.paged([kv], 16, hkv, 64, BF, seed=1)
+    k[..., 0] = float("inf")
+    q = torch.zeros(rows, hq, 64, dtype=BF, device=DEV)
+    q[..., 0] = -1.0
+    args = (table, A.starts([new]), A.ints([kv]), max_new, max_kv)
+    got = eb.attention(q, eb.KVCache(k, v), *args, mask="full")
+    assert bool((got[:new] == 0).all())
+    k[int(table[0, 2]), :, 5] = 0.0
+    got = eb.attention(q, eb.KVCache(k, v), *args, mask="full")
+    want = v[int(table[0, 2]), :, 5].repeat_interleave(hq // hkv, 0)
+    assert torch.equal(got[:new], want.expand(new, hq, 64))
+
+
+def test_rope_norm_of_tiny_heads(eb):
+    """A mean of squares below 2^-126 counts as 2^-126; one just above it is taken as it is."""
+    cache = eb.empty_kv_cache(1, 16, 1, 64, BF)
+    x = torch.full((2, 3 * 64), 2.0 ** -70, device=DEV)
+    x[1] = 2.0 ** -62
+    one = torch.ones(64, device=DEV)
+    q = eb.rope_append(x, cache, A.ints([0, 1]), None, None, 1, one, one, 0.0)
+    assert bool((q[0] == 2.0 ** -7).all()) and bool((q[1] == 1.0).all())
+    assert torch.equal(cache.k[0, 0, :2], q[:, 0])
